@@ -406,6 +406,101 @@ int tq_entropy_pack(const tq_plan* plan, const uint8_t* lengths, int64_t n, cons
 int tq_entropy_unpack(const tq_plan* plan, const uint8_t* lengths, int64_t n, const uint8_t* packed,
                       const uint64_t* row_offsets, uint8_t* idx, void* stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * Paged 8-bit KV cache: the tokens that 2 to 4 bits are too coarse for (recent tokens, prompts, whole layers), for many sequences
+ * at once.  A cache is a pool of pages of page_tokens tokens each, all KV heads in a page; a sequence owns the pages that its row
+ * of a page table names.  A block is one page of one head: its keys have one scale, its values another.
+ *
+ *   scale   s = 2^e with the least e >= -126 that holds the block's largest magnitude: max |x| <= M 2^e, M = 127 (TQ_I8) or 448
+ *           (TQ_E4M3); 0 for a block of zeros.  Powers of two, so x / s is exact and a code is x / s rounded once, half to even:
+ *           an int8 value in -127 .. 127, or the bits of an e4m3 number.  A stored element is code * s.
+ *   growth  tokens are added one after another: a later token that the scale does not hold raises it, and the block's codes are
+ *           rounded to the new scale (off by at most one step of it in all).  Writing at a page's first slot starts its blocks afresh.
+ *   NaN     a block that is given an infinity or a NaN has scale NaN from then on: all of it reads as NaN, visibly.
+ *   bounds  optional: per block and channel the largest and the smallest key code, in steps of 1 (TQ_I8) or, rounded outwards, of 4
+ *           (TQ_E4M3) scales.  tq_kv8_select ranks pages by them.
+ *
+ * The caller owns every array and keeps the lengths: tokens[b] is a device array, read by the kernels, so a captured graph follows it.
+ *   table   device int32, one row per sequence, row stride ldt >= width: entry j is the page of tokens j * page_tokens and on; -1 (or
+ *           any number outside the pool) is no page: attention passes over its tokens, appended tokens are dropped.
+ *   starts  device int32[nseq + 1], ascending: the rows of Q, K, V and out that belong to sequence b are starts[b] .. starts[b+1] - 1;
+ *           NULL: one row per sequence.  Rows behind the last sequence are neither read nor written.
+ * d is 32, 64, 96 or 128, page_tokens 16, 32, 64 or 128; row and head strides of Q, K, V and out are in elements and arbitrary (channels are
+ * contiguous).  Arrays of the cache are 16-byte aligned, the others aligned to their elements.
+ */
+enum { TQ_I8 = 0, TQ_E4M3 = 1 };               /* code_type                                   */
+typedef struct tq_kv8 {
+  uint8_t *k, *v;                /* [pages, heads, page_tokens, d] codes                       */
+  float *k_scale, *v_scale;      /* [pages, heads]                                             */
+  int8_t* k_bounds;              /* [pages, heads, 2, d] largest and smallest, or NULL         */
+  int64_t pages;
+  int heads, page_tokens, d, code_type;
+} tq_kv8;
+
+/* Writes new tokens of nseq sequences behind their tokens[b] cached ones: rows of K and V, [n rows, heads, d] of dtype TQ_F32 or
+ * TQ_BF16, row strides ldk / ldv, head strides hk / hv.  A page that is written to must belong to one sequence of the call only
+ * (tq_pages_fork gives every child a page of its own for its next tokens).  One launch; tokens is not changed. */
+int tq_kv8_append(const tq_kv8* cache, const int32_t* table, int64_t ldt, int width, int nseq, const int32_t* tokens,
+                  const int32_t* starts, int64_t n, const void* K, int64_t ldk, int64_t hk, const void* V, int64_t ldv, int64_t hv,
+                  int dtype, void* stream);
+
+/* Attention over the cache: for query head r = h * q_per_kv + j of row i of sequence b, with m rows in the sequence,
+ *     logit_t = scale <q, k_t>,  out = sum_t softmax(logit)_t v_t,  lse = log sum_t exp(logit_t)   over t < tokens[b] - (m - 1 - i):
+ * the rows are the sequence's last m tokens (tokens counts them), each sees itself and what is before it.  A row that sees nothing has
+ * out = 0 and lse = -inf.
+ *   Q, out       [n rows, heads * q_per_kv, d] of dtype, row strides ldq / ldo, head strides hq / ho; 1 <= q_per_kv <= 256.
+ *                TQ_BF16: weights are rounded to 11 bits; TQ_F32: products as exact as fp32 sums
+ *   max_queries  no sequence has more rows than this
+ *   lists        NULL, or [n, heads, nlist] int32: the numbers of the pages (entries of the sequence's row of the table) that a row
+ *                attends to, shared by the heads of a group, in any order; entries outside the sequence's pages are passed over, a
+ *                page that is listed twice counts twice
+ *   lse          [n, heads * q_per_kv] floats, or NULL
+ *   workspace    256-byte aligned, >= tq_kv8_attend_workspace_bytes(...); results do not depend on what is in it, nor on timing
+ */
+size_t tq_kv8_attend_workspace_bytes(const tq_kv8* cache, int nseq, int64_t n, int q_per_kv, int max_queries, int nlist);
+int tq_kv8_attend(const tq_kv8* cache, const int32_t* table, int64_t ldt, int width, int nseq, const int32_t* tokens,
+                  const int32_t* starts, int64_t n, int max_queries, const void* Q, int64_t ldq, int64_t hq, int q_per_kv, int dtype,
+                  float scale, const int32_t* lists, int nlist, void* out, int64_t ldo, int64_t ho, float* lse, void* workspace,
+                  size_t workspace_bytes, void* stream);
+
+/* The k pages with the best scores for every row and KV head, for tq_kv8_attend's lists: ascending page numbers, -1 behind them where
+ * the row sees fewer pages.  With qi = round(q / 2^e) in -127 .. 127 (2^e as for a block), B+ and B- the bounds in steps u s,
+ *     score(page) = max over the group's heads of 2^e u s sum_c (max(qi_c, 0) B+_c + min(qi_c, 0) B-_c),
+ * for scale > 0 no less than any logit of the page up to q's rounding.  Sums of integers and powers of two: scores are exact, and of
+ * equal ones the lower page number is taken.  The first `first` and the last `last` pages that the row sees are always taken
+ * (first + last <= k), and so is a block with scale NaN.  A query with an infinity or a NaN scores 0 everywhere.
+ *   lists      device out, [n, heads, k];  workspace  256-byte aligned, >= tq_kv8_select_workspace_bytes(cache, n, width)
+ */
+size_t tq_kv8_select_workspace_bytes(const tq_kv8* cache, int64_t n, int width);
+int tq_kv8_select(const tq_kv8* cache, const int32_t* table, int64_t ldt, int width, int nseq, const int32_t* tokens,
+                  const int32_t* starts, int64_t n, const void* Q, int64_t ldq, int64_t hq, int q_per_kv, int dtype, int first, int last,
+                  int k, int32_t* lists, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bookkeeping of the pages.  refs[p] (device int32) counts the table rows that hold page p; a page with 0 is free.  Calls take the lowest
+ * free pages, in the order of their requests, so the same calls give the same tables.  `rows` rows of the table, as above.
+ *   spare      device int32 out: free pages left; negative: so many were missing, and the last requests' entries are -1
+ *   workspace  256-byte aligned, >= tq_pages_workspace_bytes(pages, rows) (extend), (pages, count) (fork), (pages, 0) (compact)
+ *
+ * extend   gives row b the pages that next[b] tokens need beyond those of tokens[b] (up to its width; next <= tokens: none)
+ * fork     makes row children[f] a copy of row parents[f]: its full pages are shared, the page that its last tokens fill in part is
+ *          copied to one of the child's own; tokens[child] = tokens[parent].  Children are free rows (what they held is overwritten),
+ *          all different and none of them a parent; a parent may have several.  Row numbers outside the table are passed over
+ * free     the rows seqs[0 .. count-1] give back their pages; their entries become -1 and tokens 0 (tokens may be NULL)
+ * compact  moves pages to the front of the pool, as few as possible, and renames them in refs and the table (all tables that name them
+ *          must be in this one); afterwards the pages from pages - spare on are free
+ * copy     page src[i] to page dst[i] in all arrays of the cache; no dst is a src or another dst; pairs outside the pool are passed over */
+size_t tq_pages_workspace_bytes(int64_t pages, int requests);
+int tq_pages_extend(int32_t* refs, int64_t pages, int32_t* table, int64_t ldt, int width, int rows, const int32_t* tokens,
+                    const int32_t* next, int page_tokens, int32_t* spare, void* workspace, size_t workspace_bytes, void* stream);
+int tq_pages_fork(const tq_kv8* cache, int32_t* refs, int32_t* table, int64_t ldt, int width, int rows, int32_t* tokens,
+                  const int32_t* parents, const int32_t* children, int count, int32_t* spare, void* workspace, size_t workspace_bytes,
+                  void* stream);
+int tq_pages_free(int32_t* refs, int64_t pages, int32_t* table, int64_t ldt, int width, int rows, int32_t* tokens, const int32_t* seqs,
+                  int count, void* stream);
+int tq_pages_compact(const tq_kv8* cache, int32_t* refs, int32_t* table, int64_t ldt, int width, int rows, int32_t* spare,
+                     void* workspace, size_t workspace_bytes, void* stream);
+int tq_pages_copy(const tq_kv8* cache, const int32_t* src, const int32_t* dst, int count, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -11,4 +11,7 @@ from .binding import (  # noqa: F401
     TQ_LAYOUT_CANONICAL, TQ_LAYOUT_NIBBLE, tq_convert_layout, tq_query_bytes, tq_query_prepare, tq_score_prepared,
     tq_score_static_max_queries, tq_selftest_wait_timeout, tq_entropy_lengths, tq_entropy_pack, tq_entropy_unpack,
     KvGroup, tq_attend_decode, tq_attend_decode_workspace_bytes, tq_kv_append,
+    TQ_E4M3, TQ_I8, Kv8, Kv8Cache, tq_kv8_append, tq_kv8_attend, tq_kv8_attend_workspace_bytes, tq_kv8_select,
+    tq_kv8_select_workspace_bytes, tq_pages_compact, tq_pages_copy, tq_pages_extend, tq_pages_fork, tq_pages_free,
+    tq_pages_workspace_bytes,
 )

@@ -13,6 +13,7 @@ TQ_F32, TQ_BF16 = 0, 1
 TQ_ORTHOGONAL, TQ_GAUSSIAN = 0, 1
 TQ_LAYOUT_CANONICAL, TQ_LAYOUT_NIBBLE = 0, 1
 TQ_OP_QUANTIZE, TQ_OP_SCORE, TQ_OP_TOPK, TQ_OP_WSUM, TQ_OP_DEQUANTIZE = 0, 1, 2, 3, 4
+TQ_I8, TQ_E4M3 = 0, 1
 TQ_STATIC_SCRATCH_BYTES = 1 << 20
 
 # TQ_LIB_VARIANT=debug loads libtq_debug.so, the build with device-side index checks (build.py --debug)
@@ -67,6 +68,22 @@ _SIGNATURES = {
     "tq_attend_decode": (c_int, [c_void_p, c_int, c_int, c_int64, c_int64, c_int, c_void_p, c_int, c_int64, ctypes.c_float,
                                  c_void_p, c_int64, c_void_p, c_size_t, c_void_p]),
     "tq_kv_append": (c_int, [c_void_p, c_int, c_int, c_int64, c_int64, c_void_p, c_void_p, c_int, c_int64, c_int64, c_void_p]),
+    "tq_kv8_append": (c_int, [c_void_p, c_void_p, c_int64, c_int, c_int, c_void_p, c_void_p, c_int64, c_void_p, c_int64, c_int64, c_void_p,
+                              c_int64, c_int64, c_int, c_void_p]),
+    "tq_kv8_attend_workspace_bytes": (c_size_t, [c_void_p, c_int, c_int64, c_int, c_int, c_int]),
+    "tq_kv8_attend": (c_int, [c_void_p, c_void_p, c_int64, c_int, c_int, c_void_p, c_void_p, c_int64, c_int, c_void_p, c_int64, c_int64, c_int,
+                              c_int, ctypes.c_float, c_void_p, c_int, c_void_p, c_int64, c_int64, c_void_p, c_void_p, c_size_t, c_void_p]),
+    "tq_kv8_select_workspace_bytes": (c_size_t, [c_void_p, c_int64, c_int]),
+    "tq_kv8_select": (c_int, [c_void_p, c_void_p, c_int64, c_int, c_int, c_void_p, c_void_p, c_int64, c_void_p, c_int64, c_int64, c_int, c_int,
+                              c_int, c_int, c_int, c_void_p, c_void_p, c_size_t, c_void_p]),
+    "tq_pages_workspace_bytes": (c_size_t, [c_int64, c_int]),
+    "tq_pages_extend": (c_int, [c_void_p, c_int64, c_void_p, c_int64, c_int, c_int, c_void_p, c_void_p, c_int, c_void_p, c_void_p, c_size_t,
+                                c_void_p]),
+    "tq_pages_fork": (c_int, [c_void_p, c_void_p, c_void_p, c_int64, c_int, c_int, c_void_p, c_void_p, c_void_p, c_int, c_void_p, c_void_p,
+                              c_size_t, c_void_p]),
+    "tq_pages_free": (c_int, [c_void_p, c_int64, c_void_p, c_int64, c_int, c_int, c_void_p, c_void_p, c_int, c_void_p]),
+    "tq_pages_compact": (c_int, [c_void_p, c_void_p, c_void_p, c_int64, c_int, c_int, c_void_p, c_void_p, c_size_t, c_void_p]),
+    "tq_pages_copy": (c_int, [c_void_p, c_void_p, c_void_p, c_int, c_void_p]),
 }
 
 
@@ -75,6 +92,12 @@ class KvGroup(ctypes.Structure):
     lib().tq_attend_decode / tq_kv_append themselves; the functions below take mappings."""
     _fields_ = [(name, c_void_p) for name in ("plan_k", "plan_v", "k_idx", "k_qjl", "k_gamma", "k_norms", "v_idx", "v_norms",
                                               "k_channels", "v_channels")]
+
+
+class Kv8(ctypes.Structure):
+    """struct tq_kv8 of include/tq.h (a paged 8-bit KV cache), for programs that call lib() themselves; Kv8Cache owns one."""
+    _fields_ = [(name, c_void_p) for name in ("k", "v", "k_scale", "v_scale", "k_bounds")] + [("pages", c_int64)] + [
+        (name, c_int) for name in ("heads", "page_tokens", "d", "code_type")]
 
 
 class TqError(RuntimeError):
@@ -313,3 +336,91 @@ def tq_entropy_unpack(plan: Plan, lengths, n: int, packed, offsets, idx_out):
 
 def tq_select_topk(cand_scores, cand_ids, k: int, top_scores, top_ids):
     _check((_n or _native()).select_topk(cand_scores, cand_ids, k, top_scores, top_ids))
+
+
+_KV8_TYPES = {torch.int8: TQ_I8, torch.float8_e4m3fn: TQ_E4M3}
+
+
+class Kv8Cache:
+    """A paged 8-bit KV cache over tensors of the caller: k, v [pages, heads, page_tokens, d] of torch.int8 or torch.float8_e4m3fn,
+    k_scale, v_scale [pages, heads] float32 and, for tq_kv8_select, k_bounds [pages, heads, 2, d] int8; all contiguous."""
+
+    def __init__(self, k, v, k_scale, v_scale, k_bounds=None):
+        if k.dim() != 4 or k.dtype not in _KV8_TYPES:
+            raise ValueError("k must be [pages, heads, page_tokens, d] of torch.int8 or torch.float8_e4m3fn")
+        pages, heads, page_tokens, d = k.shape
+        wanted = [("k", k, k.shape, k.dtype), ("v", v, k.shape, k.dtype), ("k_scale", k_scale, (pages, heads), torch.float32),
+                  ("v_scale", v_scale, (pages, heads), torch.float32)]
+        if k_bounds is not None:
+            wanted.append(("k_bounds", k_bounds, (pages, heads, 2, d), torch.int8))
+        for name, t, shape, dtype in wanted:
+            if not t.is_cuda or t.device != k.device:
+                raise ValueError("expected CUDA tensors of one device (this library has no CPU path)")
+            if tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous():
+                raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}")
+        self.k, self.v, self.k_scale, self.v_scale, self.k_bounds = k, v, k_scale, v_scale, k_bounds
+        self.pages, self.heads, self.page_tokens, self.d = pages, heads, page_tokens, d
+        self._struct = Kv8(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(),
+                           None if k_bounds is None else k_bounds.data_ptr(), pages, heads, page_tokens, d, _KV8_TYPES[k.dtype])
+        self.handle = ctypes.addressof(self._struct)
+        self.device_index = k.device.index
+
+    @classmethod
+    def empty(cls, pages: int, heads: int, page_tokens: int, d: int, dtype=torch.int8, bounds: bool = True, device="cuda"):
+        """A cache whose pages hold nothing yet."""
+        new = lambda *shape, dtype: torch.zeros(shape, dtype=dtype, device=device)
+        return cls(new(pages, heads, page_tokens, d, dtype=dtype), new(pages, heads, page_tokens, d, dtype=dtype),
+                   new(pages, heads, dtype=torch.float32), new(pages, heads, dtype=torch.float32),
+                   new(pages, heads, 2, d, dtype=torch.int8) if bounds else None)
+
+
+def tq_kv8_append(cache: Kv8Cache, table, tokens, K, V, starts=None):
+    """Quantises new tokens (rows of K, V: [n, heads, d]) into the pages behind the tokens[b] cached ones of every sequence."""
+    _check((_n or _native()).kv8_append(cache, table, tokens, starts, K, V))
+
+
+def tq_kv8_attend_workspace_bytes(cache: Kv8Cache, nseq: int, n: int, q_per_kv: int, max_queries: int = 1, nlist: int = 0) -> int:
+    return lib().tq_kv8_attend_workspace_bytes(cache.handle, nseq, n, q_per_kv, max_queries, nlist)
+
+
+def tq_kv8_attend(cache: Kv8Cache, table, tokens, Q, scale: float, out, workspace, lse=None, starts=None, max_queries: int = 1, lists=None):
+    """Attention of Q [n, heads * q_per_kv, d] over the sequences' caches (or, with lists [n, heads, nlist], over the listed pages)."""
+    _check((_n or _native()).kv8_attend(cache, table, tokens, starts, Q, scale, out, lse, max_queries, lists, workspace))
+
+
+def tq_kv8_select_workspace_bytes(cache: Kv8Cache, n: int, width: int) -> int:
+    return lib().tq_kv8_select_workspace_bytes(cache.handle, n, width)
+
+
+def tq_kv8_select(cache: Kv8Cache, table, tokens, Q, lists, workspace, starts=None, first: int = 1, last: int = 1):
+    """The lists.shape[2] best pages of every row and KV head into lists [n, heads, k] (int32), for tq_kv8_attend."""
+    _check((_n or _native()).kv8_select(cache, table, tokens, starts, Q, first, last, lists, workspace))
+
+
+def tq_pages_workspace_bytes(pages: int, requests: int) -> int:
+    return lib().tq_pages_workspace_bytes(pages, requests)
+
+
+def tq_pages_extend(refs, table, tokens, next_tokens, page_tokens: int, spare, workspace):
+    """Gives every row of the table the pages that next_tokens[b] need beyond those of tokens[b]."""
+    _check((_n or _native()).pages_extend(refs, table, tokens, next_tokens, page_tokens, spare, workspace))
+
+
+def tq_pages_fork(cache: Kv8Cache, refs, table, tokens, parents, children, spare, workspace):
+    """Makes row children[f] a copy of row parents[f]: full pages shared, the last one in part copied."""
+    _check((_n or _native()).pages_fork(cache, refs, table, tokens, parents, children, spare, workspace))
+
+
+def tq_pages_free(refs, table, tokens, seqs):
+    """The rows seqs give back their pages."""
+    _check((_n or _native()).pages_free(refs, table, tokens, seqs))
+
+
+def tq_pages_compact(cache: Kv8Cache, refs, table, spare, workspace):
+    """Moves the pages in use to the front of the pool and renames them in refs and table."""
+    _check((_n or _native()).pages_compact(cache, refs, table, spare, workspace))
+
+
+def tq_pages_copy(cache: Kv8Cache, src, dst):
+    """Page src[i] to page dst[i], in all arrays of the cache."""
+    _check((_n or _native()).pages_copy(cache, src, dst))

@@ -6,6 +6,7 @@
 #include <dlfcn.h>
 
 #include <ATen/ATen.h>
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -18,7 +19,9 @@ struct Api {
 #define TQ_API_LIST(X)                                                                                                   \
   X(tq_quantize_mse) X(tq_quantize_prod) X(tq_dequantize) X(tq_score) X(tq_score_static) X(tq_query_prepare)             \
   X(tq_score_prepared) X(tq_topk) X(tq_select_topk) X(tq_wsum) X(tq_softmax) X(tq_attend_decode) X(tq_kv_append)         \
-  X(tq_entropy_workspace_bytes) X(tq_entropy_measure) X(tq_entropy_pack) X(tq_entropy_unpack)
+  X(tq_entropy_workspace_bytes) X(tq_entropy_measure) X(tq_entropy_pack) X(tq_entropy_unpack)                       \
+  X(tq_kv8_append) X(tq_kv8_attend) X(tq_kv8_select) X(tq_pages_extend) X(tq_pages_fork) X(tq_pages_free)                \
+  X(tq_pages_compact) X(tq_pages_copy)
   TQ_API_LIST(TQ_API)
 } api;
 
@@ -342,6 +345,204 @@ TQ_FN(kv_append, 6) {   // groups, heads, head_stride, position, K, V
   return run([&] { return api.tq_kv_append(g.g, g.n, heads, stride, position, k.p, v.p, dt, k.ld, v.ld, st); });
 }
 
+// ---- paged 8-bit cache: shapes, types and devices are checked here, where the tensors are known
+struct Cache8 {
+  const tq_kv8* c;
+  int64_t device;
+};
+PyObject* device_name;
+Cache8 cache8(PyObject* o) {
+  PyObject* h = PyObject_GetAttr(o, handle_name);
+  if (h == nullptr) throw Failed();
+  const void* p = PyLong_AsVoidPtr(h);
+  Py_DECREF(h);
+  if (p == nullptr) {
+    if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "the cache has no handle");
+    throw Failed();
+  }
+  PyObject* d = PyObject_GetAttr(o, device_name);
+  if (d == nullptr) throw Failed();
+  const long long dev = PyLong_AsLongLong(d);
+  Py_DECREF(d);
+  if (dev == -1 && PyErr_Occurred()) throw Failed();
+  if (dev != c10::cuda::current_device()) fail("the cache is not on the current device");
+  return {static_cast<const tq_kv8*>(p), dev};
+}
+const at::Tensor& on_device(PyObject* o) {
+  const at::Tensor& t = tensor(o);
+  if (!t.is_cuda()) fail("expected a CUDA tensor (this library has no CPU path)");
+  if (t.device().index() != c10::cuda::current_device()) fail("a tensor is not on the current device");
+  return t;
+}
+// A contiguous int32 vector of n entries (n < 0: any number), or NULL for None.
+int32_t* ints(PyObject* o, int64_t n, const char* what) {
+  if (o == Py_None) return nullptr;
+  const at::Tensor& t = on_device(o);
+  if (t.scalar_type() != at::kInt || t.dim() != 1 || !t.is_contiguous() || (n >= 0 && t.size(0) != n)) {
+    PyErr_Format(PyExc_ValueError, n >= 0 ? "%s must be a contiguous int32 vector of %lld entries" : "%s must be a contiguous int32 vector", what, (long long)n);
+    throw Failed();
+  }
+  return t.data_ptr<int32_t>();
+}
+struct PageTable {
+  int32_t* p;
+  int64_t ld;
+  int width, rows;
+};
+PageTable page_table(PyObject* o) {
+  const at::Tensor& t = on_device(o);
+  if (t.scalar_type() != at::kInt || t.dim() != 2 || (t.size(1) > 1 && t.stride(1) != 1)) fail("table must be a 2-D int32 tensor with unit inner stride");
+  if (t.size(0) > INT32_MAX || t.size(1) > INT32_MAX) fail("table is too large");
+  return {t.data_ptr<int32_t>(), t.size(0) > 1 ? t.stride(0) : std::max<int64_t>(t.stride(0), t.size(1)), (int)t.size(1), (int)t.size(0)};
+}
+// [n, heads, d] with contiguous channels; heads a multiple of the cache's.
+struct Heads {
+  void* p;
+  int64_t n, row, head;
+  int heads, dtype;
+};
+Heads heads_of(PyObject* o, const Cache8& c, const char* what) {
+  const at::Tensor& t = on_device(o);
+  if (t.dim() != 3 || t.size(2) != c.c->d || t.stride(2) != 1 || t.size(1) == 0 || t.size(1) % c.c->heads != 0) {
+    PyErr_Format(PyExc_ValueError, "%s must be [rows, heads, %d] with contiguous channels, heads a multiple of the cache's %d", what, c.c->d, c.c->heads);
+    throw Failed();
+  }
+  int dtype = TQ_F32;
+  if (t.scalar_type() == at::kBFloat16) dtype = TQ_BF16;
+  else if (t.scalar_type() != at::kFloat) fail("unsupported dtype: expected torch.float32 or torch.bfloat16");
+  return {t.data_ptr(), t.size(0), t.stride(0), t.stride(1), (int)t.size(1), dtype};
+}
+
+TQ_FN(kv8_append, 6) {   // cache, table, tokens, starts, K, V
+  const Cache8 c = cache8(a[0]);
+  const PageTable t = page_table(a[1]);
+  const int32_t* tokens = ints(a[2], t.rows, "tokens");
+  const int32_t* starts = ints(a[3], (int64_t)t.rows + 1, "starts");
+  const Heads k = heads_of(a[4], c, "K"), v = heads_of(a[5], c, "V");
+  if (k.n != v.n || k.heads != c.c->heads || v.heads != c.c->heads || k.dtype != v.dtype) fail("K and V must have one shape, [rows, heads, d], and one dtype");
+  void* st = stream();
+  return run([&] {
+    return api.tq_kv8_append(c.c, t.p, t.ld, t.width, t.rows, tokens, starts, k.n, k.p, k.row, k.head, v.p, v.row, v.head, k.dtype, st);
+  });
+}
+
+// [n, heads, k] contiguous int32
+int32_t* page_lists(PyObject* o, int64_t n, int heads, int* k) {
+  const at::Tensor& t = on_device(o);
+  if (t.scalar_type() != at::kInt || t.dim() != 3 || t.size(0) != n || t.size(1) != heads || !t.is_contiguous() || t.size(2) > INT32_MAX)
+    fail("lists must be a contiguous int32 tensor [rows, KV heads, pages]");
+  *k = (int)t.size(2);
+  return t.data_ptr<int32_t>();
+}
+
+TQ_FN(kv8_attend, 11) {   // cache, table, tokens, starts, Q, scale, out, lse, max_queries, lists, workspace
+  const Cache8 c = cache8(a[0]);
+  const PageTable t = page_table(a[1]);
+  const int32_t* tokens = ints(a[2], t.rows, "tokens");
+  const int32_t* starts = ints(a[3], (int64_t)t.rows + 1, "starts");
+  const Heads q = heads_of(a[4], c, "Q"), o = heads_of(a[6], c, "out");
+  if (q.n != o.n || q.heads != o.heads || q.dtype != o.dtype) fail("out must have the shape and dtype of Q");
+  const float scale = (float)real(a[5]);
+  float* lse = nullptr;
+  if (a[7] != Py_None) {
+    const at::Tensor& l = on_device(a[7]);
+    if (l.scalar_type() != at::kFloat || l.dim() != 2 || l.size(0) != q.n || l.size(1) != q.heads || !l.is_contiguous())
+      fail("lse must be a contiguous float32 tensor [rows, heads]");
+    lse = l.data_ptr<float>();
+  }
+  const int max_queries = int32(a[8]);
+  int nlist = 0;
+  const int32_t* lists = a[9] == Py_None ? nullptr : page_lists(a[9], q.n, c.c->heads, &nlist);
+  if (a[10] != Py_None) on_device(a[10]);
+  const Bytes w = scratch(a[10]);
+  void* st = stream();
+  return run([&] {
+    return api.tq_kv8_attend(c.c, t.p, t.ld, t.width, t.rows, tokens, starts, q.n, max_queries, q.p, q.row, q.head, q.heads / c.c->heads, q.dtype, scale,
+                             lists, nlist, o.p, o.row, o.head, lse, w.p, w.n, st);
+  });
+}
+
+TQ_FN(kv8_select, 9) {   // cache, table, tokens, starts, Q, first, last, lists, workspace
+  const Cache8 c = cache8(a[0]);
+  const PageTable t = page_table(a[1]);
+  const int32_t* tokens = ints(a[2], t.rows, "tokens");
+  const int32_t* starts = ints(a[3], (int64_t)t.rows + 1, "starts");
+  const Heads q = heads_of(a[4], c, "Q");
+  const int first = int32(a[5]), last = int32(a[6]);
+  int k = 0;
+  int32_t* lists = page_lists(a[7], q.n, c.c->heads, &k);
+  if (a[8] != Py_None) on_device(a[8]);
+  const Bytes w = scratch(a[8]);
+  void* st = stream();
+  return run([&] {
+    return api.tq_kv8_select(c.c, t.p, t.ld, t.width, t.rows, tokens, starts, q.n, q.p, q.row, q.head, q.heads / c.c->heads, q.dtype, first, last, k, lists,
+                             w.p, w.n, st);
+  });
+}
+
+int vector_size(PyObject* o) {
+  const at::Tensor& t = tensor(o);
+  if (t.dim() != 1 || t.size(0) > INT32_MAX) fail("expected an int32 vector");
+  return (int)t.size(0);
+}
+
+TQ_FN(pages_extend, 7) {   // refs, table, tokens, next, page_tokens, spare, workspace
+  int32_t* refs = ints(a[0], -1, "refs");
+  const PageTable t = page_table(a[1]);
+  const int32_t *tokens = ints(a[2], t.rows, "tokens"), *next = ints(a[3], t.rows, "next_tokens");
+  const int page = int32(a[4]);
+  int32_t* spare = ints(a[5], 1, "spare");
+  if (a[6] != Py_None) on_device(a[6]);
+  const Bytes w = scratch(a[6]);
+  const int64_t pages = vector_size(a[0]);
+  void* st = stream();
+  return run([&] { return api.tq_pages_extend(refs, pages, t.p, t.ld, t.width, t.rows, tokens, next, page, spare, w.p, w.n, st); });
+}
+
+TQ_FN(pages_fork, 8) {   // cache, refs, table, tokens, parents, children, spare, workspace
+  const Cache8 c = cache8(a[0]);
+  int32_t* refs = ints(a[1], c.c->pages, "refs");
+  const PageTable t = page_table(a[2]);
+  int32_t* tokens = ints(a[3], t.rows, "tokens");
+  const int count = vector_size(a[4]);
+  const int32_t *parents = ints(a[4], count, "parents"), *children = ints(a[5], count, "children");
+  int32_t* spare = ints(a[6], 1, "spare");
+  if (a[7] != Py_None) on_device(a[7]);
+  const Bytes w = scratch(a[7]);
+  void* st = stream();
+  return run([&] { return api.tq_pages_fork(c.c, refs, t.p, t.ld, t.width, t.rows, tokens, parents, children, count, spare, w.p, w.n, st); });
+}
+
+TQ_FN(pages_free, 4) {   // refs, table, tokens, seqs
+  int32_t* refs = ints(a[0], -1, "refs");
+  const PageTable t = page_table(a[1]);
+  int32_t* tokens = ints(a[2], t.rows, "tokens");
+  const int count = vector_size(a[3]);
+  const int32_t* seqs = ints(a[3], count, "seqs");
+  const int64_t pages = vector_size(a[0]);
+  void* st = stream();
+  return run([&] { return api.tq_pages_free(refs, pages, t.p, t.ld, t.width, t.rows, tokens, seqs, count, st); });
+}
+
+TQ_FN(pages_compact, 5) {   // cache, refs, table, spare, workspace
+  const Cache8 c = cache8(a[0]);
+  int32_t* refs = ints(a[1], c.c->pages, "refs");
+  const PageTable t = page_table(a[2]);
+  int32_t* spare = ints(a[3], 1, "spare");
+  if (a[4] != Py_None) on_device(a[4]);
+  const Bytes w = scratch(a[4]);
+  void* st = stream();
+  return run([&] { return api.tq_pages_compact(c.c, refs, t.p, t.ld, t.width, t.rows, spare, w.p, w.n, st); });
+}
+
+TQ_FN(pages_copy, 3) {   // cache, src, dst
+  const Cache8 c = cache8(a[0]);
+  const int count = vector_size(a[1]);
+  const int32_t *src = ints(a[1], count, "src"), *dst = ints(a[2], count, "dst");
+  void* st = stream();
+  return run([&] { return api.tq_pages_copy(c.c, src, dst, count, st); });
+}
+
 // Measures, reads the total back and packs.  Returns (packed, offsets), or the failed call's status.
 TQ_FN(entropy_pack, 4) {   // plan, lengths (host address), n, idx
   const tq_plan* p = plan_of(a[0]);
@@ -408,6 +609,8 @@ PyMethodDef methods[] = {{"bind", bind, METH_O, nullptr},
                          TQ_DEF(quantize_mse), TQ_DEF(quantize_prod), TQ_DEF(dequantize), TQ_DEF(score), TQ_DEF(score_static),
                          TQ_DEF(query_prepare), TQ_DEF(score_prepared), TQ_DEF(topk), TQ_DEF(select_topk), TQ_DEF(wsum),
                          TQ_DEF(softmax), TQ_DEF(attend_decode), TQ_DEF(kv_append), TQ_DEF(entropy_pack), TQ_DEF(entropy_unpack),
+                         TQ_DEF(kv8_append), TQ_DEF(kv8_attend), TQ_DEF(kv8_select), TQ_DEF(pages_extend), TQ_DEF(pages_fork),
+                         TQ_DEF(pages_free), TQ_DEF(pages_compact), TQ_DEF(pages_copy),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tqbind", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
@@ -418,5 +621,6 @@ PyMODINIT_FUNC PyInit__tqbind() {
   for (int i = 0; i < kKeys; ++i)
     if ((keys[i] = PyUnicode_InternFromString(names[i])) == nullptr) return nullptr;
   if ((handle_name = PyUnicode_InternFromString("handle")) == nullptr) return nullptr;
+  if ((device_name = PyUnicode_InternFromString("device_index")) == nullptr) return nullptr;
   return PyModule_Create(&module);
 }

@@ -1,0 +1,731 @@
+// Attention over a paged 8-bit KV cache for few queries per sequence (decoding, drafted tokens, listed pages).
+//
+// Mathematics.  Columns are the queries that share a KV head (q_per_kv heads of up to a few tokens, 8 or 16 at a time); per 16 tokens
+//   S^T = K Q^T   (16 tokens x 8 columns, one mma per 16 channels: the codes are the A operand, converted to fp16 exactly),
+//   p = 2^(s - m + 6) with the column's running maximum m,   O^T += V^T P^T   (P^T is S^T transposed in registers).
+// m only moves when a score exceeds it by 2^8, so most steps rescale nothing; p <= 2^14 stays inside fp16.
+// Queries are scaled per row by a power of two into [2^13, 2^14): bf16 values are then exact in fp16 (an element 2^-30 of the row's
+// largest loses bits), and fp32 values are two fp16 limbs (2^-23 of each value).  P is one fp16 limb for bf16 outputs (2^-12 of each
+// weight, an eighth of the output's own rounding) and two for fp32 ones.  All sums are fp32.
+// Scales are powers of two: the key's goes into the score's factor, the value's into p, relative to a unit u of the accumulator that
+// follows the largest scale (exact; P keeps its bits while scales stay within 2^4 of u, and u moves where they do not).
+//
+// Work.  Units of 64 tokens of one (sequence, head) are numbered through; every CTA takes an equal share of them, whatever the lengths,
+// and of a unit each of its four warps takes 16 tokens, straight from global memory into registers, one step ahead.  Warps are
+// independent until their share of an item ends; items that several CTAs share are joined by a second, dependent launch in a fixed order.
+#include <algorithm>
+#include <cstring>
+
+#include "tq_kv8.h"
+#include "tq_kv8_attend.h"
+
+namespace tq {
+namespace kv8 {
+namespace {
+
+constexpr int kWarps = 4, kThreads = kWarps * 32;
+constexpr int kUnit = 64;                // tokens
+constexpr float kLift = 6.f, kSlack = 8.f;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+#define TQ_INF __uint_as_float(0x7F800000u)
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t half2_bits(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+// Bytes 0, 1 and bytes 2, 3 of a word of codes as pairs of fp16, exactly.  int8: the byte plus 128 is the low byte of 1024 + 128 + x.
+template <bool E4M3>
+__device__ __forceinline__ void expand(uint32_t w, uint32_t& lo, uint32_t& hi) {
+  if (E4M3) {
+    const __half2_raw a = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w & 0xFFFFu), __NV_E4M3);
+    const __half2_raw b = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w >> 16), __NV_E4M3);
+    lo = (uint32_t)a.x | ((uint32_t)a.y << 16);
+    hi = (uint32_t)b.x | ((uint32_t)b.y << 16);
+  } else {
+    w ^= 0x80808080u;
+    const uint32_t a = __byte_perm(w, 0x64646464u, 0x4140), b = __byte_perm(w, 0x64646464u, 0x4342);
+    const __half2 k = __halves2half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480));   // 1152
+    const __half2 x = __hsub2(*reinterpret_cast<const __half2*>(&a), k), y = __hsub2(*reinterpret_cast<const __half2*>(&b), k);
+    lo = *reinterpret_cast<const uint32_t*>(&x);
+    hi = *reinterpret_cast<const uint32_t*>(&y);
+  }
+}
+
+template <int W>
+__device__ __forceinline__ void load_words(const uint8_t* p, uint32_t* w) {   // W words, aligned to the largest power of two in their bytes
+  if (W % 4 == 0) {
+#pragma unroll
+    for (int i = 0; i < W / 4; ++i) {
+      const uint4 v = __ldg(reinterpret_cast<const uint4*>(p) + i);
+      w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
+    }
+  } else if (W % 2 == 0) {
+#pragma unroll
+    for (int i = 0; i < W / 2; ++i) {
+      const uint2 v = __ldg(reinterpret_cast<const uint2*>(p) + i);
+      w[2 * i] = v.x; w[2 * i + 1] = v.y;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < W; ++i) w[i] = __ldg(reinterpret_cast<const uint32_t*>(p) + i);
+  }
+}
+
+// Units of sequence b (all heads and column blocks).  Sequences whose queries go to the many-query kernel have none here.
+struct Shape {
+  int64_t begin, end, tokens;   // rows, cached tokens
+  int blocks;                   // blocks of NC columns
+  int64_t units;                // of one (head, block)
+};
+__device__ __forceinline__ Shape shape_of(const AttendArgs& a, int b, int nc) {
+  Shape s;
+  rows_of(a.b, b, &s.begin, &s.end);
+  s.tokens = tokens_of(a.b, b, a.c.page_shift);
+  const int64_t cols = (s.end - s.begin) * a.g;
+  s.blocks = cols > a.most_cols ? 0 : (int)((cols + nc - 1) / nc);
+  s.units = s.blocks == 0 ? 0 : max((s.tokens + kUnit - 1) / kUnit, (int64_t)1);   // without tokens: one, for the zeros
+  return s;
+}
+
+__device__ __forceinline__ int64_t block_total(int64_t v, int64_t* sums, int64_t* upto) {   // inclusive sum in order, and the total
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int64_t s = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int64_t y = __shfl_up_sync(0xffffffffu, s, o);
+    if (lane >= o) s += y;
+  }
+  __syncthreads();
+  if (lane == 31) sums[warp] = s;
+  __syncthreads();
+  int64_t all = 0;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) {
+    if (w < warp) s += sums[w];
+    all += sums[w];
+  }
+  *upto = s;
+  return all;
+}
+
+template <typename T, int D, bool E4M3, int NT>
+struct Kernel {
+  static constexpr int kLimbs = sizeof(T) == 4 ? 2 : 1;
+  static constexpr int NC = 8 * NT;
+  static constexpr int KW = D / 16;                       // words of a key row per lane
+  static constexpr int KS = D % 64 == 0 ? 4 : 2;          // ... in pieces of that many
+  static constexpr int VW = D / 32;                       // words of a value row per lane
+  static constexpr int QP = D + 8;                        // pitch of the queries in shared memory, halves
+  static constexpr int OP = D + 4;                        // pitch of the warps' results, floats
+  static constexpr size_t q_bytes = sizeof(__half) * kLimbs * NC * QP;
+  static constexpr size_t o_bytes = sizeof(float) * kWarps * NC * OP;
+  static constexpr size_t smem = (q_bytes > o_bytes ? q_bytes : o_bytes) + sizeof(float) * (2 * kWarps + 3) * NC + 256;
+};
+
+template <typename T>
+__device__ __forceinline__ void store_out(T* p, float x);
+template <>
+__device__ __forceinline__ void store_out<float>(float* p, float x) { *p = x; }
+template <>
+__device__ __forceinline__ void store_out<__nv_bfloat16>(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
+
+template <typename T, int D, bool E4M3, int NT>
+__global__ void __launch_bounds__(kThreads) attend_kernel(const __grid_constant__ AttendArgs a) {
+  using K = Kernel<T, D, E4M3, NT>;
+  constexpr int NC = K::NC, KW = K::KW, KS = K::KS, VW = K::VW, LIMBS = K::kLimbs;
+  extern __shared__ uint4 smem4[];
+  __half* qsm = reinterpret_cast<__half*>(smem4);
+  float* osm = reinterpret_cast<float*>(smem4);
+  float* msm = reinterpret_cast<float*>(reinterpret_cast<char*>(smem4) + (K::q_bytes > K::o_bytes ? K::q_bytes : K::o_bytes));   // [warps][NC]
+  float* lsm = msm + kWarps * NC;
+  float* fsm = lsm + kWarps * NC;       // [NC] factor of a column's scores
+  float* top = fsm + NC;                // [NC] maximum, then sum, of all warps
+  float* tot = top + NC;
+  int64_t* sums = reinterpret_cast<int64_t*>(tot + NC);   // [8]
+  int* found = reinterpret_cast<int*>(sums + 8);
+  const int t = threadIdx.x, lane = t & 31, warp = t >> 5, c4 = lane & 3, n8 = lane >> 2;
+  const int cta = blockIdx.x;
+  allow_successor();
+  wait_for_predecessor();
+
+  // ---- this CTA's share [u, u_end) of all units, and the item that u falls into
+  int seq = 0, head = 0, block = 0;
+  int64_t item_at = 0;                  // first unit of the item
+  int64_t total = 0, per;
+  Shape sh;
+  int64_t list_units = 0;
+  const int T_ = 1 << a.c.page_shift;
+  if (a.lists == nullptr) {
+    int64_t upto = 0, own = 0;
+    for (int b0 = 0; b0 < a.b.nseq; b0 += kThreads) {
+      own = 0;
+      if (b0 + t < a.b.nseq) {
+        const Shape s = shape_of(a, b0 + t, NC);
+        own = s.units * s.blocks * a.c.heads;
+      }
+      total += block_total(own, sums, &upto);
+    }
+    per = max((total + gridDim.x - 1) / gridDim.x, (int64_t)1);
+    const int64_t u0 = (int64_t)cta * per;
+    if (u0 < total) {
+      int64_t before = 0;
+      for (int b0 = 0;; b0 += kThreads) {
+        int64_t all = total;
+        if (a.b.nseq > kThreads) {
+          own = 0;
+          if (b0 + t < a.b.nseq) {
+            const Shape s = shape_of(a, b0 + t, NC);
+            own = s.units * s.blocks * a.c.heads;
+          }
+          all = block_total(own, sums, &upto);
+        }
+        if (before + all > u0) {
+          const int64_t from = before + upto - own;
+          if (own > 0 && from <= u0 && u0 < from + own) {
+            found[0] = b0 + t;
+            sums[6] = from;
+          }
+          __syncthreads();
+          break;
+        }
+        before += all;
+      }
+      seq = found[0];
+      const int64_t from = sums[6];
+      sh = shape_of(a, seq, NC);
+      const int64_t i = (u0 - from) / sh.units;
+      head = (int)(i / sh.blocks);
+      block = (int)(i % sh.blocks);
+      item_at = from + i * sh.units;
+    }
+  } else {                               // rows x heads x blocks of columns, each of as many units as a list holds
+    int64_t rows = a.b.nseq;
+    if (a.b.starts != nullptr) {
+      rows = a.b.starts[a.b.nseq];
+      rows = rows < 0 ? 0 : (rows > a.b.n ? a.b.n : rows);
+    }
+    sh.blocks = (a.g + NC - 1) / NC;
+    list_units = max((((int64_t)a.nlist << a.c.page_shift) + kUnit - 1) / kUnit, (int64_t)1);
+    total = rows * a.c.heads * sh.blocks * list_units;
+    per = max((total + gridDim.x - 1) / gridDim.x, (int64_t)1);
+    const int64_t i = (int64_t)cta * per / list_units;
+    seq = (int)(i / ((int64_t)a.c.heads * sh.blocks));          // a row here
+    head = (int)(i / sh.blocks % a.c.heads);
+    block = (int)(i % sh.blocks);
+    item_at = i * list_units;
+  }
+  int64_t u = (int64_t)cta * per;
+  const int64_t u_end = min(total, u + per);
+  Meta* meta = a.meta + cta;
+  if (t == 0) meta->last_cta = -1;
+  if (u >= u_end) return;
+
+  while (u < u_end) {
+    // ---- the item: rows, columns, what each column sees
+    int64_t row0, tokens, units;
+    int b = seq, cols, width_c = a.g;    // columns of a row
+    int64_t len_q;
+    const int32_t* list = nullptr;
+    if (a.lists == nullptr) {
+      row0 = sh.begin;
+      len_q = sh.end - sh.begin;
+      tokens = sh.tokens;
+      cols = (int)min(len_q * a.g - (int64_t)block * NC, (int64_t)NC);
+      units = sh.units;
+    } else {
+      row0 = seq;
+      len_q = 1;
+      int64_t visible;
+      row_info(a.b, row0, a.c.page_shift, &b, &visible);
+      tokens = b < 0 ? 0 : visible;
+      cols = b < 0 ? 0 : min(a.g - block * NC, NC);   // a row of no sequence is left as it was
+      units = list_units;
+      list = a.lists + (row0 * a.c.heads + head) * a.nlist;
+    }
+    const int col0 = block * NC;
+    const int64_t u_stop = min(u_end, item_at + units);
+    // ---- queries: scaled to [2^13, 2^14) per column, as fp16 limbs
+    for (int j = warp; j < NC; j += kWarps) {
+      const int jc = col0 + j;
+      const T* q = static_cast<const T*>(a.q) + (row0 + jc / width_c) * a.ldq + (int64_t)(head * a.g + jc % width_c) * a.hq;
+      float x[D / 32];
+      uint32_t most = 0u;
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i) {
+        x[i] = j < cols ? (float)q[i * 32 + lane] : 0.f;
+        most = max(most, __float_as_uint(x[i]) & 0x7FFFFFFFu);
+      }
+      most = __reduce_max_sync(0xffffffffu, most);
+      // 2^e with e such that most * 2^-e is in [2^13, 2^14); 13 below the exponent of most, kept normal
+      const int e = min(max((int)(most >> 23) - 13, 1), 253);
+      const float s = __uint_as_float((uint32_t)e << 23), inv = __uint_as_float((uint32_t)(254 - e) << 23);
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i) {
+        const float y = x[i] * inv;
+        const __half hi = __float2half_rn(y);
+        qsm[j * K::QP + i * 32 + lane] = hi;
+        if (LIMBS == 2) qsm[(NC + j) * K::QP + i * 32 + lane] = __float2half_rn(y - __half2float(hi));
+      }
+      // a row with an infinity or a NaN has no scores: NaN
+      if (lane == 0) fsm[j] = most >= 0x7F800000u ? __uint_as_float(0x7FC00000u) : s * (a.scale * kLog2e);
+    }
+    __syncthreads();
+    float f[NT][2];
+    int vis[NT][2];                       // tokens that the column sees
+    int vis_min = (int)min(tokens, (int64_t)INT32_MAX), vis_max = vis_min;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int j = nt * 8 + 2 * c4 + e;
+        f[nt][e] = fsm[j];
+        vis[nt][e] = j < cols && a.lists == nullptr ? (int)max(tokens - (len_q - 1 - (col0 + j) / width_c), (int64_t)0) : vis_max;
+      }
+    if (a.lists == nullptr) {
+      vis_min = (int)max(tokens - (len_q - 1 - col0 / width_c), (int64_t)0);
+      vis_max = (int)max(tokens - (len_q - 1 - (col0 + cols - 1) / width_c), (int64_t)0);
+    }
+    uint32_t qf[NT * LIMBS == 1 ? KW : 1][2];
+    if (NT * LIMBS == 1) {
+#pragma unroll
+      for (int w = 0; w < KW; ++w) {
+        const uint2 y = *reinterpret_cast<const uint2*>(qsm + n8 * K::QP + 4 * KS * 4 * (w / KS) + 4 * KS * c4 + 4 * (w % KS));
+        qf[w][0] = y.x;
+        qf[w][1] = y.y;
+      }
+    }
+
+    float m[NT][2], l[NT][2], o[2 * VW][NT][4];
+    float unit = 0.f, last_vs = 0.f, ratio = 0.f;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      m[nt][0] = m[nt][1] = -TQ_INF;
+      l[nt][0] = l[nt][1] = 0.f;
+#pragma unroll
+      for (int j = 0; j < 2 * VW; ++j) o[j][nt][0] = o[j][nt][1] = o[j][nt][2] = o[j][nt][3] = 0.f;
+    }
+
+    struct Group { int id, t0; };         // page and first token of 16, id < 0: nothing there
+    auto resolve = [&](int64_t i) -> Group {
+      Group r{-1, 0};
+      if (i >= u_stop) return r;
+      const int64_t s = (i - item_at) * kUnit + warp * 16;      // place in the sequence, or in the pages of the list one after another
+      int64_t lp = s >> a.c.page_shift;
+      if (list != nullptr) lp = lp < a.nlist ? list[lp] : -1;
+      if (lp < 0) return r;
+      const int64_t t0 = (lp << a.c.page_shift) + (s & (T_ - 1));
+      if (t0 >= vis_max) return r;
+      r.t0 = (int)t0;
+      r.id = page_of(a.b, a.c.pages, b, lp);
+      return r;
+    };
+    struct Tile {
+      uint32_t k[2][KW], v[4][VW];
+      float ks, vs;
+      Group g;
+    };
+    auto load = [&](const Group& g, Tile& x) {
+      x.g = g;
+      if (g.id < 0) return;
+      const int64_t blk = (int64_t)g.id * a.c.heads + head;
+      const int64_t at = ((blk << a.c.page_shift) + (g.t0 & (T_ - 1))) * D;
+      x.ks = __ldg(a.c.k_scale + blk);
+      x.vs = __ldg(a.c.v_scale + blk);
+#pragma unroll
+      for (int r = 0; r < 2; ++r)
+#pragma unroll
+        for (int i = 0; i < KW / KS; ++i) load_words<KS>(a.c.k + at + (n8 + 8 * r) * D + 16 * KS * i + 4 * KS * c4, &x.k[r][KS * i]);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) load_words<VW>(a.c.v + at + (2 * c4 + (r & 1) + 8 * (r >> 1)) * D + 4 * VW * n8, x.v[r]);
+    };
+    auto compute = [&](Tile& x) {
+      if (x.g.id < 0) return;
+      float s[NT][4];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
+#pragma unroll
+      for (int w = 0; w < KW; ++w) {
+        uint32_t y[4];
+        expand<E4M3>(x.k[0][w], y[0], y[2]);
+        expand<E4M3>(x.k[1][w], y[1], y[3]);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int li = 0; li < LIMBS; ++li) {
+            if (NT * LIMBS == 1) {
+              mma_f16(s[nt], y, qf[w][0], qf[w][1]);
+            } else {
+              const uint2 z = *reinterpret_cast<const uint2*>(qsm + (li * NC + nt * 8 + n8) * K::QP + 16 * KS * (w / KS) + 4 * KS * c4 + 4 * (w % KS));
+              mma_f16(s[nt], y, z.x, z.y);
+            }
+          }
+      }
+      const bool edge = x.g.t0 + 16 > vis_min;      // some column does not see all 16 tokens
+      bool higher = false;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[nt][e] *= f[nt][e & 1] * x.ks;
+        if (edge) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (x.g.t0 + n8 + 8 * (e >> 1) >= vis[nt][e & 1]) s[nt][e] = -TQ_INF;
+        }
+        higher |= fmaxf(s[nt][0], s[nt][2]) > m[nt][0] + kSlack || fmaxf(s[nt][1], s[nt][3]) > m[nt][1] + kSlack;
+      }
+      if (__any_sync(0xffffffffu, higher)) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            float g = fmaxf(s[nt][e], s[nt][2 + e]);
+            g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, 4));
+            g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, 8));
+            g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, 16));
+            const float top_m = fmaxf(m[nt][e], g);
+            const float alpha = top_m > m[nt][e] ? ex2(m[nt][e] - top_m) : 1.f;    // m = -inf: 0
+            m[nt][e] = top_m;
+            l[nt][e] *= alpha;
+#pragma unroll
+            for (int j = 0; j < 2 * VW; ++j) {
+              o[j][nt][e] *= alpha;
+              o[j][nt][2 + e] *= alpha;
+            }
+          }
+      }
+      if (x.vs != last_vs) {                        // the unit of the accumulators follows the largest scale
+        last_vs = x.vs;
+        if (!(x.vs == x.vs)) {
+          ratio = x.vs;
+          last_vs = 0.f;                            // NaN: looked at again for the next tile
+        } else if (x.vs == 0.f) {
+          ratio = 0.f;
+        } else if (unit == 0.f || x.vs > unit || (x.vs < unit * 0.0625f && unit < x.vs * 1e18f)) {
+          const float back = unit / x.vs;
+#pragma unroll
+          for (int j = 0; j < 2 * VW; ++j)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) o[j][nt][e] *= back;
+          unit = x.vs;
+          ratio = 1.f;
+        } else {
+          ratio = x.vs / unit;
+        }
+      } else if (x.vs == 0.f) {
+        ratio = 0.f;
+      }
+      uint32_t p[NT][LIMBS][2];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        float y[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float mm = m[nt][e & 1];
+          y[e] = ex2(s[nt][e] + (mm == -TQ_INF ? 0.f : kLift - mm));
+          l[nt][e & 1] += y[e];
+          y[e] = edge && y[e] == 0.f ? 0.f : y[e] * ratio;    // what a column does not see adds nothing, NaN or not
+        }
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const uint32_t hi = half2_bits(y[2 * r], y[2 * r + 1]);
+          p[nt][0][r] = transpose8(hi);
+          if (LIMBS == 2) {
+            const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&hi));
+            p[nt][LIMBS - 1][r] = transpose8(half2_bits(y[2 * r] - back.x, y[2 * r + 1] - back.y));
+          }
+        }
+      }
+      if (edge && E4M3) {                           // slots behind the last token may hold codes of NaN
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (x.g.t0 + 2 * c4 + (r & 1) + 8 * (r >> 1) >= vis_max) {
+#pragma unroll
+            for (int j = 0; j < VW; ++j) x.v[r][j] = 0u;
+          }
+      }
+#pragma unroll
+      for (int j = 0; j < VW; ++j) {
+        uint32_t lo[4], hi[4];                      // of channel 4 j, 4 j + 1 and of 4 j + 2, 4 j + 3
+        expand<E4M3>(__byte_perm(x.v[0][j], x.v[1][j], 0x5140), lo[0], lo[1]);
+        expand<E4M3>(__byte_perm(x.v[2][j], x.v[3][j], 0x5140), lo[2], lo[3]);
+        expand<E4M3>(__byte_perm(x.v[0][j], x.v[1][j], 0x7362), hi[0], hi[1]);
+        expand<E4M3>(__byte_perm(x.v[2][j], x.v[3][j], 0x7362), hi[2], hi[3]);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int li = 0; li < LIMBS; ++li) {
+            mma_f16(o[2 * j][nt], lo, p[nt][li][0], p[nt][li][1]);
+            mma_f16(o[2 * j + 1][nt], hi, p[nt][li][0], p[nt][li][1]);
+          }
+      }
+    };
+    {
+      Tile x, y;
+      load(resolve(u), x);
+      Group next = resolve(u + 1);
+      for (int64_t i = u; i < u_stop; i += 2) {
+        load(next, y);
+        next = resolve(i + 2);
+        compute(x);
+        load(next, x);
+        next = resolve(i + 3);
+        compute(y);
+      }
+    }
+
+    // ---- the four warps' results as one
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float z = l[nt][e];
+        z += __shfl_xor_sync(0xffffffffu, z, 4);
+        z += __shfl_xor_sync(0xffffffffu, z, 8);
+        z += __shfl_xor_sync(0xffffffffu, z, 16);
+        if (n8 == 0) {
+          msm[warp * NC + nt * 8 + 2 * c4 + e] = m[nt][e];
+          lsm[warp * NC + nt * 8 + 2 * c4 + e] = z;
+        }
+      }
+    __syncthreads();                       // queries have been read, maxima are there
+    if (t < NC) {
+      float best = -TQ_INF, sum = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) best = fmaxf(best, msm[w * NC + t]);
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) sum += lsm[w * NC + t] * (best == -TQ_INF ? 1.f : ex2(msm[w * NC + t] - best));
+      top[t] = best;
+      tot[t] = sum;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int j = nt * 8 + 2 * c4 + e;
+        const float w = (top[j] == -TQ_INF ? 1.f : ex2(m[nt][e] - top[j])) * unit;
+#pragma unroll
+        for (int i = 0; i < 2 * VW; ++i) {
+          osm[(warp * NC + j) * K::OP + 4 * VW * n8 + 2 * i] = o[i][nt][e] * w;
+          osm[(warp * NC + j) * K::OP + 4 * VW * n8 + 2 * i + 1] = o[i][nt][2 + e] * w;
+        }
+      }
+    __syncthreads();
+    const bool whole = u == item_at && u_stop == item_at + units;
+    const int slot = 2 * cta + (u == item_at ? 1 : 0);
+    for (int i = t; i < cols * D; i += kThreads) {
+      const int j = i / D, ch = i % D;
+      float y = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) y += osm[(w * NC + j) * K::OP + ch];
+      if (whole) {
+        const int jc = col0 + j;
+        T* out = static_cast<T*>(a.out) + (row0 + jc / width_c) * a.ldo + (int64_t)(head * a.g + jc % width_c) * a.ho;
+        store_out<T>(out + ch, tot[j] == 0.f ? 0.f : y / tot[j]);
+      } else {
+        a.part_o[((int64_t)slot * kMaxCols + j) * D + ch] = y;
+      }
+    }
+    if (t < cols) {
+      if (whole) {
+        const int jc = col0 + t;
+        if (a.lse) a.lse[(row0 + jc / width_c) * ((int64_t)a.c.heads * a.g) + head * a.g + jc % width_c] =
+            tot[t] == 0.f ? -TQ_INF : (top[t] == -TQ_INF ? 0.f : (top[t] - kLift) * kLn2) + logf(tot[t]);
+      } else {
+        a.part_ml[(int64_t)slot * 2 * kMaxCols + t] = top[t];
+        a.part_ml[(int64_t)slot * 2 * kMaxCols + kMaxCols + t] = tot[t];
+      }
+    }
+    if (!whole && u == item_at && t == 0) {
+      meta->row0 = (int)row0;
+      meta->col0 = col0;
+      meta->cols = cols;
+      meta->head = head;
+      meta->last_cta = (int)((item_at + units - 1) / per);
+    }
+    __syncthreads();                       // shared memory is the next item's
+    // ---- the next item
+    u = u_stop;
+    item_at += units;
+    if (u < u_end && ++block == sh.blocks) {
+      block = 0;
+      if (++head == a.c.heads) {
+        head = 0;
+        ++seq;
+        if (a.lists == nullptr)
+          for (sh = shape_of(a, seq, NC); sh.units == 0; sh = shape_of(a, seq, NC)) ++seq;   // u < total: there is one
+      }
+    }
+  }
+}
+
+// Joins the parts of the item that began in CTA blockIdx.x's share, in the order of the shares.
+template <typename T, int D>
+__global__ void __launch_bounds__(kThreads) join_kernel(const __grid_constant__ AttendArgs a) {
+  __shared__ float w_s[kThreads];
+  __shared__ float red_m[kWarps], red_l[kWarps];
+  wait_for_predecessor();
+  const Meta z = a.meta[blockIdx.x];
+  const int j = blockIdx.y, t = threadIdx.x, lane = t & 31, warp = t >> 5;
+  if (z.last_cta < 0 || j >= z.cols) return;
+  const int first = blockIdx.x, parts = z.last_cta - first + 1;
+  auto slot = [&](int i) { return 2 * (first + i) + (i == 0 ? 1 : 0); };
+  float best = -TQ_INF;
+  for (int i = t; i < parts; i += kThreads) best = fmaxf(best, a.part_ml[(int64_t)slot(i) * 2 * kMaxCols + j]);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, o));
+  if (lane == 0) red_m[warp] = best;
+  __syncthreads();
+  best = fmaxf(fmaxf(red_m[0], red_m[1]), fmaxf(red_m[2], red_m[3]));
+  float sum = 0.f, y = 0.f;
+  for (int i0 = 0; i0 < parts; i0 += kThreads) {
+    const int n = min(parts - i0, kThreads);
+    float wl = 0.f;
+    __syncthreads();
+    if (t < n) {
+      const float* ml = a.part_ml + (int64_t)slot(i0 + t) * 2 * kMaxCols + j;
+      const float w = best == -TQ_INF ? 1.f : ex2(ml[0] - best);
+      w_s[t] = w;
+      wl = ml[kMaxCols] * w;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) wl += __shfl_xor_sync(0xffffffffu, wl, o);
+    if (lane == 0) red_l[warp] = wl;
+    __syncthreads();
+    sum += (red_l[0] + red_l[1]) + (red_l[2] + red_l[3]);
+    if (t < D) {
+      const float* po = a.part_o + (int64_t)j * D + t;
+#pragma unroll 8
+      for (int i = 0; i < n; ++i) y = fmaf(po[(int64_t)slot(i0 + i) * kMaxCols * D], w_s[i], y);
+    }
+  }
+  const int jc = z.col0 + j, g = a.g;
+  const int64_t row = (int64_t)z.row0 + jc / g;
+  const int head = z.head * g + jc % g;
+  if (t < D) store_out<T>(static_cast<T*>(a.out) + row * a.ldo + (int64_t)head * a.ho + t, sum == 0.f ? 0.f : y / sum);
+  if (t == 0 && a.lse) a.lse[row * ((int64_t)a.c.heads * g) + head] =
+      sum == 0.f ? -TQ_INF : (best == -TQ_INF ? 0.f : (best - kLift) * kLn2) + logf(sum);
+}
+
+template <typename T, int D, bool E4M3, int NT>
+cudaError_t launch(const AttendArgs& a, int grid, cudaStream_t st) {
+  static std::atomic<unsigned long long> devices{0};
+  const cudaError_t e = allow_largest_smem(reinterpret_cast<const void*>(attend_kernel<T, D, E4M3, NT>), devices);
+  if (e != cudaSuccess) return e;
+  return launch_dependent(attend_kernel<T, D, E4M3, NT>, dim3((unsigned)grid), dim3(kThreads), Kernel<T, D, E4M3, NT>::smem, st, a);
+}
+template <typename T, int D>
+cudaError_t launch_d(const AttendArgs& a, bool e4m3, int nt, int grid, cudaStream_t st) {
+  cudaError_t e;
+  if (e4m3) e = nt == 1 ? launch<T, D, true, 1>(a, grid, st) : launch<T, D, true, 2>(a, grid, st);
+  else e = nt == 1 ? launch<T, D, false, 1>(a, grid, st) : launch<T, D, false, 2>(a, grid, st);
+  if (e != cudaSuccess) return e;
+  return launch_dependent(join_kernel<T, D>, dim3((unsigned)grid, (unsigned)(8 * nt)), dim3(kThreads), 0, st, a);
+}
+template <typename T>
+cudaError_t launch_t(const AttendArgs& a, bool e4m3, int nt, int grid, cudaStream_t st) {
+  switch (a.c.d) {
+    case 32: return launch_d<T, 32>(a, e4m3, nt, grid, st);
+    case 64: return launch_d<T, 64>(a, e4m3, nt, grid, st);
+    case 96: return launch_d<T, 96>(a, e4m3, nt, grid, st);
+    default: return launch_d<T, 128>(a, e4m3, nt, grid, st);
+  }
+}
+
+constexpr int kCtasPerSm = 3;
+
+struct Space {
+  size_t meta, ml, o, bytes;
+};
+Space lay_out(int grid, int d) {
+  Space s;
+  s.meta = 0;
+  s.ml = (size_t)round_up64((int64_t)grid * sizeof(Meta), 256);
+  s.o = s.ml + (size_t)round_up64((int64_t)grid * 2 * 2 * kMaxCols * sizeof(float), 256);
+  s.bytes = s.o + (size_t)round_up64((int64_t)grid * 2 * kMaxCols * d * sizeof(float), 256);
+  return s;
+}
+
+}  // namespace
+
+size_t attend_space(int sms, int d) { return lay_out(sms * kCtasPerSm, d).bytes; }
+
+cudaError_t launch_attend(AttendArgs& a, int dtype, bool e4m3, int cols, int sms, void* workspace, cudaStream_t st) {
+  const int grid = sms * kCtasPerSm;
+  const Space s = lay_out(grid, a.c.d);
+  char* w = static_cast<char*>(workspace);
+  a.meta = reinterpret_cast<Meta*>(w + s.meta);
+  a.part_ml = reinterpret_cast<float*>(w + s.ml);
+  a.part_o = reinterpret_cast<float*>(w + s.o);
+  const int nt = cols <= 8 ? 1 : 2;
+  return dtype == TQ_F32 ? launch_t<float>(a, e4m3, nt, grid, st) : launch_t<__nv_bfloat16>(a, e4m3, nt, grid, st);
+}
+
+}  // namespace kv8
+}  // namespace tq
+
+extern "C" size_t tq_kv8_attend_workspace_bytes(const tq_kv8* cache, int nseq, int64_t n, int q_per_kv, int max_queries, int nlist) {
+  using namespace tq;
+  using namespace tq::kv8;
+  int dev = 0, sms = 0;
+  if (cache == nullptr || cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+  (void)nseq; (void)n; (void)q_per_kv; (void)max_queries; (void)nlist;
+  return attend_space(sms, cache->d);
+}
+
+extern "C" int tq_kv8_attend(const tq_kv8* cache, const int32_t* table, int64_t ldt, int width, int nseq, const int32_t* tokens,
+                             const int32_t* starts, int64_t n, int max_queries, const void* Q, int64_t ldq, int64_t hq, int q_per_kv,
+                             int dtype, float scale, const int32_t* lists, int nlist, void* out, int64_t ldo, int64_t ho, float* lse,
+                             void* workspace, size_t workspace_bytes, void* stream) {
+  using namespace tq;
+  using namespace tq::kv8;
+  const char* who = "tq_kv8_attend";
+  TQ_RANGE(who);
+  AttendArgs a;
+  std::memset(&a, 0, sizeof(a));
+  int rc = check_cache(who, cache, &a.c);
+  if (rc == TQ_OK) rc = check_batch(who, table, ldt, width, nseq, tokens, starts, n, &a.b);
+  if (rc != TQ_OK) return rc;
+  TQ_REQUIRE(dtype == TQ_F32 || dtype == TQ_BF16, TQ_ERR_UNSUPPORTED, "%s: unknown dtype %d", who, dtype);
+  TQ_REQUIRE(q_per_kv >= 1 && q_per_kv <= 256, TQ_ERR_UNSUPPORTED, "%s: 1..256 queries per KV head", who);
+  TQ_REQUIRE(max_queries >= 0 && nlist >= 0, TQ_ERR_INVALID_ARG, "%s: negative size", who);
+  TQ_REQUIRE(starts != nullptr || max_queries >= 1, TQ_ERR_INVALID_ARG, "%s: max_queries is 0 where every sequence has one row", who);
+  TQ_REQUIRE(lists != nullptr || nlist == 0, TQ_ERR_INVALID_ARG, "%s: lists is NULL", who);
+  TQ_REQUIRE(nlist <= (1 << 24), TQ_ERR_UNSUPPORTED, "%s: lists of %d pages", who, nlist);
+  if (nseq == 0 || n == 0 || max_queries == 0) return TQ_OK;
+  TQ_REQUIRE(Q != nullptr && out != nullptr, TQ_ERR_INVALID_ARG, "%s: Q or out is NULL", who);
+  TQ_REQUIRE(ldq >= 0 && hq >= 0 && ldo >= 0 && ho >= 0, TQ_ERR_INVALID_ARG, "%s: negative stride", who);
+  const uintptr_t align = dtype == TQ_F32 ? 3 : 1;
+  TQ_REQUIRE(((reinterpret_cast<uintptr_t>(Q) | reinterpret_cast<uintptr_t>(out)) & align) == 0 && (reinterpret_cast<uintptr_t>(lse) & 3) == 0,
+             TQ_ERR_ALIGNMENT, "%s: Q, out or lse is not aligned to its elements", who);
+  const size_t need = tq_kv8_attend_workspace_bytes(cache, nseq, n, q_per_kv, max_queries, nlist);
+  TQ_REQUIRE(workspace != nullptr && workspace_bytes >= need, TQ_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", who, workspace_bytes, need);
+  TQ_REQUIRE((reinterpret_cast<uintptr_t>(workspace) & 255) == 0, TQ_ERR_ALIGNMENT, "%s: workspace is not 256-byte aligned", who);
+  int dev = 0, sms = 0;
+  TQ_CHECK_CUDA(cudaGetDevice(&dev), who);
+  TQ_CHECK_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev), who);
+  a.q = Q; a.ldq = ldq; a.hq = hq; a.g = q_per_kv; a.scale = scale;
+  a.lists = lists; a.nlist = nlist; a.out = out; a.ldo = ldo; a.ho = ho; a.lse = lse;
+  a.most_cols = INT32_MAX;
+  const int64_t cols = lists ? q_per_kv : (int64_t)max_queries * q_per_kv;
+  TQ_CHECK_CUDA(launch_attend(a, dtype, cache->code_type == TQ_E4M3, (int)std::min<int64_t>(cols, 16), sms, workspace, static_cast<cudaStream_t>(stream)), who);
+  count_launches(2);
+  return TQ_OK;
+}

@@ -11,7 +11,7 @@
 // follows the largest scale (exact; P keeps its bits while scales stay within 2^4 of u, and u moves where they do not).
 //
 // Work.  Units of 64 tokens of one (sequence, head) are numbered through; every CTA takes an equal share of them, whatever the lengths,
-// and of a unit each of its four warps takes 16 tokens, straight from global memory into registers, one step ahead.  Warps are
+// and of a unit each of its four warps takes 16 tokens, through a ring of its own in shared memory, some steps ahead.  Warps are
 // independent until their share of an item ends; items that several CTAs share are joined by a second, dependent launch in a fixed order.
 #include <algorithm>
 #include <cstring>
@@ -71,19 +71,34 @@ __device__ __forceinline__ void load_words(const uint8_t* p, uint32_t* w) {   //
   if (W % 4 == 0) {
 #pragma unroll
     for (int i = 0; i < W / 4; ++i) {
-      const uint4 v = __ldg(reinterpret_cast<const uint4*>(p) + i);
+      const uint4 v = reinterpret_cast<const uint4*>(p)[i];
       w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
     }
   } else if (W % 2 == 0) {
 #pragma unroll
     for (int i = 0; i < W / 2; ++i) {
-      const uint2 v = __ldg(reinterpret_cast<const uint2*>(p) + i);
+      const uint2 v = reinterpret_cast<const uint2*>(p)[i];
       w[2 * i] = v.x; w[2 * i + 1] = v.y;
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < W; ++i) w[i] = __ldg(reinterpret_cast<const uint32_t*>(p) + i);
+    for (int i = 0; i < W; ++i) w[i] = reinterpret_cast<const uint32_t*>(p)[i];
   }
+}
+__device__ __forceinline__ void copy16(uint32_t to, const void* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copy4(uint32_t to, const void* from) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(from) : "memory");
+}
+// Where 16-byte chunk x of row r of a warp's tile is kept: the lanes of a phase of the reads below then touch different banks.
+template <int D>
+__device__ __forceinline__ int key_chunk(int r, int x) {
+  return r * (D / 16) + (D == 128 ? x ^ ((r & 1) << 2) : x);
+}
+template <int D>
+__device__ __forceinline__ int value_chunk(int r, int x) {
+  return r * (D / 16) + (D == 128 ? x ^ (r & 6) : (D == 64 ? x ^ (r & 2) : x));
 }
 
 // Units of sequence b (all heads and column blocks).  Sequences whose queries go to the many-query kernel have none here.
@@ -132,9 +147,15 @@ struct Kernel {
   static constexpr int VW = D / 32;                       // words of a value row per lane
   static constexpr int QP = D + 8;                        // pitch of the queries in shared memory, halves
   static constexpr int OP = D + 4;                        // pitch of the warps' results, floats
+  static constexpr int kTile = 2 * 16 * D + 16;           // bytes of a warp's stage: keys, values, the two scales
+  static constexpr int kStages = D >= 96 ? 4 : 5;
+  // 168 registers a thread and a ring of 66 KB let three CTAs share an SM; two fp16 limbs of 16 columns need more
+  static constexpr int kCtas = D >= 96 && NT == 2 && kLimbs == 2 ? 2 : 3;
   static constexpr size_t q_bytes = sizeof(__half) * kLimbs * NC * QP;
   static constexpr size_t o_bytes = sizeof(float) * kWarps * NC * OP;
-  static constexpr size_t smem = (q_bytes > o_bytes ? q_bytes : o_bytes) + sizeof(float) * (2 * kWarps + 3) * NC + 256;
+  static constexpr size_t ring = (size_t)kWarps * kStages * kTile;
+  static constexpr size_t head = ring > o_bytes ? ring : o_bytes;   // the results take the ring's place
+  static constexpr size_t smem = head + q_bytes + sizeof(float) * (2 * kWarps + 3) * NC + 256;
 };
 
 template <typename T>
@@ -145,13 +166,13 @@ template <>
 __device__ __forceinline__ void store_out<__nv_bfloat16>(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
 
 template <typename T, int D, bool E4M3, int NT>
-__global__ void __launch_bounds__(kThreads) attend_kernel(const __grid_constant__ AttendArgs a) {
+__global__ void __launch_bounds__(kThreads, Kernel<T, D, E4M3, NT>::kCtas) attend_kernel(const __grid_constant__ AttendArgs a) {
   using K = Kernel<T, D, E4M3, NT>;
   constexpr int NC = K::NC, KW = K::KW, KS = K::KS, VW = K::VW, LIMBS = K::kLimbs;
   extern __shared__ uint4 smem4[];
-  __half* qsm = reinterpret_cast<__half*>(smem4);
   float* osm = reinterpret_cast<float*>(smem4);
-  float* msm = reinterpret_cast<float*>(reinterpret_cast<char*>(smem4) + (K::q_bytes > K::o_bytes ? K::q_bytes : K::o_bytes));   // [warps][NC]
+  __half* qsm = reinterpret_cast<__half*>(reinterpret_cast<char*>(smem4) + K::head);
+  float* msm = reinterpret_cast<float*>(reinterpret_cast<char*>(qsm) + K::q_bytes);   // [warps][NC]
   float* lsm = msm + kWarps * NC;
   float* fsm = lsm + kWarps * NC;       // [NC] factor of a column's scores
   float* top = fsm + NC;                // [NC] maximum, then sum, of all warps
@@ -320,49 +341,56 @@ __global__ void __launch_bounds__(kThreads) attend_kernel(const __grid_constant_
       for (int j = 0; j < 2 * VW; ++j) o[j][nt][0] = o[j][nt][1] = o[j][nt][2] = o[j][nt][3] = 0.f;
     }
 
-    struct Group { int id, t0; };         // page and first token of 16, id < 0: nothing there
-    auto resolve = [&](int64_t i) -> Group {
-      Group r{-1, 0};
-      if (i >= u_stop) return r;
-      const int64_t s = (i - item_at) * kUnit + warp * 16;      // place in the sequence, or in the pages of the list one after another
-      int64_t lp = s >> a.c.page_shift;
-      if (list != nullptr) lp = lp < a.nlist ? list[lp] : -1;
+    // place s in the sequence, or in the listed pages one after another -> logical page, or -1
+    const int i_first = (int)(u - item_at), i_stop = (int)(u_stop - item_at);   // of the item's units
+    auto entry = [&](int i) -> int {
+      if (i >= i_stop) return -1;
+      const int lp = (int)(((int64_t)i * kUnit + warp * 16) >> a.c.page_shift);
+      if (list == nullptr) return lp;
+      return lp < a.nlist ? list[lp] : -1;
+    };
+    struct Group { int id, t0; };         // page and first token of 16 tokens; t0 < 0: nothing there
+    auto resolve = [&](int i, int lp) -> Group {
+      Group r{-1, -1};
       if (lp < 0) return r;
-      const int64_t t0 = (lp << a.c.page_shift) + (s & (T_ - 1));
+      const int64_t t0 = ((int64_t)lp << a.c.page_shift) + ((i * kUnit + warp * 16) & (T_ - 1));
       if (t0 >= vis_max) return r;
-      r.t0 = (int)t0;
       r.id = page_of(a.b, a.c.pages, b, lp);
+      r.t0 = r.id < 0 ? -1 : (int)t0;
       return r;
     };
-    struct Tile {
-      uint32_t k[2][KW], v[4][VW];
-      float ks, vs;
-      Group g;
+    uint8_t* ring = reinterpret_cast<uint8_t*>(smem4) + warp * K::kStages * K::kTile;
+    auto issue = [&](const Group& g, int stage) {
+      if (g.t0 >= 0) {
+        const int64_t blk = (int64_t)g.id * a.c.heads + head;
+        const int64_t at = ((blk << a.c.page_shift) + (g.t0 & (T_ - 1))) * D;
+        const uint32_t to = (uint32_t)__cvta_generic_to_shared(ring + stage * K::kTile);
+#pragma unroll
+        for (int x = lane; x < D; x += 32) copy16(to + 16 * key_chunk<D>(x / (D / 16), x % (D / 16)), a.c.k + at + 16 * x);
+#pragma unroll
+        for (int x = lane; x < D; x += 32) copy16(to + 16 * D + 16 * value_chunk<D>(x / (D / 16), x % (D / 16)), a.c.v + at + 16 * x);
+        if (lane < 2) copy4(to + 32 * D + 4 * lane, (lane ? a.c.v_scale : a.c.k_scale) + blk);
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    auto load = [&](const Group& g, Tile& x) {
-      x.g = g;
-      if (g.id < 0) return;
-      const int64_t blk = (int64_t)g.id * a.c.heads + head;
-      const int64_t at = ((blk << a.c.page_shift) + (g.t0 & (T_ - 1))) * D;
-      x.ks = __ldg(a.c.k_scale + blk);
-      x.vs = __ldg(a.c.v_scale + blk);
-#pragma unroll
-      for (int r = 0; r < 2; ++r)
-#pragma unroll
-        for (int i = 0; i < KW / KS; ++i) load_words<KS>(a.c.k + at + (n8 + 8 * r) * D + 16 * KS * i + 4 * KS * c4, &x.k[r][KS * i]);
-#pragma unroll
-      for (int r = 0; r < 4; ++r) load_words<VW>(a.c.v + at + (2 * c4 + (r & 1) + 8 * (r >> 1)) * D + 4 * VW * n8, x.v[r]);
-    };
-    auto compute = [&](Tile& x) {
-      if (x.g.id < 0) return;
+    auto compute = [&](int t0, int stage) {
+      if (t0 < 0) return;
+      const uint8_t* tile = ring + stage * K::kTile;
+      const float ks = *reinterpret_cast<const float*>(tile + 32 * D), vs = *reinterpret_cast<const float*>(tile + 32 * D + 4);
       float s[NT][4];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
+      uint32_t kw[2][KW];
+#pragma unroll
+      for (int r = 0; r < 2; ++r)
+#pragma unroll
+        for (int i = 0; i < KW / KS; ++i)
+          load_words<KS>(tile + (KS == 4 ? 16 * key_chunk<D>(n8 + 8 * r, 4 * i + c4) : (n8 + 8 * r) * D + 32 * i + 8 * c4), &kw[r][KS * i]);
 #pragma unroll
       for (int w = 0; w < KW; ++w) {
         uint32_t y[4];
-        expand<E4M3>(x.k[0][w], y[0], y[2]);
-        expand<E4M3>(x.k[1][w], y[1], y[3]);
+        expand<E4M3>(kw[0][w], y[0], y[2]);
+        expand<E4M3>(kw[1][w], y[1], y[3]);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -375,16 +403,16 @@ __global__ void __launch_bounds__(kThreads) attend_kernel(const __grid_constant_
             }
           }
       }
-      const bool edge = x.g.t0 + 16 > vis_min;      // some column does not see all 16 tokens
+      const bool edge = t0 + 16 > vis_min;      // some column does not see all 16 tokens
       bool higher = false;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[nt][e] *= f[nt][e & 1] * x.ks;
+        for (int e = 0; e < 4; ++e) s[nt][e] *= f[nt][e & 1] * ks;
         if (edge) {
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            if (x.g.t0 + n8 + 8 * (e >> 1) >= vis[nt][e & 1]) s[nt][e] = -TQ_INF;
+            if (t0 + n8 + 8 * (e >> 1) >= vis[nt][e & 1]) s[nt][e] = -TQ_INF;
         }
         higher |= fmaxf(s[nt][0], s[nt][2]) > m[nt][0] + kSlack || fmaxf(s[nt][1], s[nt][3]) > m[nt][1] + kSlack;
       }
@@ -408,27 +436,27 @@ __global__ void __launch_bounds__(kThreads) attend_kernel(const __grid_constant_
             }
           }
       }
-      if (x.vs != last_vs) {                        // the unit of the accumulators follows the largest scale
-        last_vs = x.vs;
-        if (!(x.vs == x.vs)) {
-          ratio = x.vs;
+      if (vs != last_vs) {                        // the unit of the accumulators follows the largest scale
+        last_vs = vs;
+        if (!(vs == vs)) {
+          ratio = vs;
           last_vs = 0.f;                            // NaN: looked at again for the next tile
-        } else if (x.vs == 0.f) {
+        } else if (vs == 0.f) {
           ratio = 0.f;
-        } else if (unit == 0.f || x.vs > unit || (x.vs < unit * 0.0625f && unit < x.vs * 1e18f)) {
-          const float back = unit / x.vs;
+        } else if (unit == 0.f || vs > unit || (vs < unit * 0.0625f && unit < vs * 1e18f)) {
+          const float back = unit / vs;
 #pragma unroll
           for (int j = 0; j < 2 * VW; ++j)
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
               for (int e = 0; e < 4; ++e) o[j][nt][e] *= back;
-          unit = x.vs;
+          unit = vs;
           ratio = 1.f;
         } else {
-          ratio = x.vs / unit;
+          ratio = vs / unit;
         }
-      } else if (x.vs == 0.f) {
+      } else if (vs == 0.f) {
         ratio = 0.f;
       }
       uint32_t p[NT][LIMBS][2];
@@ -452,21 +480,28 @@ __global__ void __launch_bounds__(kThreads) attend_kernel(const __grid_constant_
           }
         }
       }
+      uint32_t vw[4][VW];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int row = 2 * c4 + (r & 1) + 8 * (r >> 1);
+        load_words<VW>(tile + 16 * D + (VW == 4 ? 16 * value_chunk<D>(row, n8)
+                                                : (VW == 2 ? 16 * value_chunk<D>(row, n8 >> 1) + 8 * (n8 & 1) : row * D + 4 * VW * n8)), vw[r]);
+      }
       if (edge && E4M3) {                           // slots behind the last token may hold codes of NaN
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-          if (x.g.t0 + 2 * c4 + (r & 1) + 8 * (r >> 1) >= vis_max) {
+          if (t0 + 2 * c4 + (r & 1) + 8 * (r >> 1) >= vis_max) {
 #pragma unroll
-            for (int j = 0; j < VW; ++j) x.v[r][j] = 0u;
+            for (int j = 0; j < VW; ++j) vw[r][j] = 0u;
           }
       }
 #pragma unroll
       for (int j = 0; j < VW; ++j) {
         uint32_t lo[4], hi[4];                      // of channel 4 j, 4 j + 1 and of 4 j + 2, 4 j + 3
-        expand<E4M3>(__byte_perm(x.v[0][j], x.v[1][j], 0x5140), lo[0], lo[1]);
-        expand<E4M3>(__byte_perm(x.v[2][j], x.v[3][j], 0x5140), lo[2], lo[3]);
-        expand<E4M3>(__byte_perm(x.v[0][j], x.v[1][j], 0x7362), hi[0], hi[1]);
-        expand<E4M3>(__byte_perm(x.v[2][j], x.v[3][j], 0x7362), hi[2], hi[3]);
+        expand<E4M3>(__byte_perm(vw[0][j], vw[1][j], 0x5140), lo[0], lo[1]);
+        expand<E4M3>(__byte_perm(vw[2][j], vw[3][j], 0x5140), lo[2], lo[3]);
+        expand<E4M3>(__byte_perm(vw[0][j], vw[1][j], 0x7362), hi[0], hi[1]);
+        expand<E4M3>(__byte_perm(vw[2][j], vw[3][j], 0x7362), hi[2], hi[3]);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -477,17 +512,35 @@ __global__ void __launch_bounds__(kThreads) attend_kernel(const __grid_constant_
       }
     };
     {
-      Tile x, y;
-      load(resolve(u), x);
-      Group next = resolve(u + 1);
-      for (int64_t i = u; i < u_stop; i += 2) {
-        load(next, y);
-        next = resolve(i + 2);
-        compute(x);
-        load(next, x);
-        next = resolve(i + 3);
-        compute(y);
+      constexpr int S = K::kStages;
+      int t0s[S - 1];                      // first tokens of the steps in flight
+      int lps[S + 1];
+#pragma unroll
+      for (int i = 0; i < S + 1; ++i) lps[i] = entry(i_first + i);
+      Group gs[S];
+#pragma unroll
+      for (int i = 0; i < S; ++i) gs[i] = resolve(i_first + i, lps[i]);
+#pragma unroll
+      for (int i = 0; i < S - 1; ++i) {
+        issue(gs[i], i);
+        t0s[i] = gs[i].t0;
       }
+      Group next = gs[S - 1];
+      int lp = lps[S], stage = 0;
+      for (int i = i_first; i < i_stop; ++i) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(S - 2) : "memory");
+        __syncwarp();                      // the step's bytes are there for all lanes, and the last step's have been read
+        const int t0 = t0s[0];
+        issue(next, stage == 0 ? S - 1 : stage - 1);
+#pragma unroll
+        for (int j = 0; j < S - 2; ++j) t0s[j] = t0s[j + 1];
+        t0s[S - 2] = next.t0;
+        next = resolve(i + S, lp);
+        lp = entry(i + S + 1);
+        compute(t0, stage);
+        stage = stage == S - 1 ? 0 : stage + 1;
+      }
+      asm volatile("cp.async.wait_group 0;" ::: "memory");
     }
 
     // ---- the four warps' results as one
@@ -504,7 +557,7 @@ __global__ void __launch_bounds__(kThreads) attend_kernel(const __grid_constant_
           lsm[warp * NC + nt * 8 + 2 * c4 + e] = z;
         }
       }
-    __syncthreads();                       // queries have been read, maxima are there
+    __syncthreads();                       // tiles have been read, maxima are there
     if (t < NC) {
       float best = -TQ_INF, sum = 0.f;
 #pragma unroll
@@ -625,31 +678,33 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const __grid_constant__ 
 }
 
 template <typename T, int D, bool E4M3, int NT>
-cudaError_t launch(const AttendArgs& a, int grid, cudaStream_t st) {
+cudaError_t launch(const AttendArgs& a, int sms, int* grid_out, cudaStream_t st) {
+  const int grid = *grid_out = sms * Kernel<T, D, E4M3, NT>::kCtas;
   static std::atomic<unsigned long long> devices{0};
   const cudaError_t e = allow_largest_smem(reinterpret_cast<const void*>(attend_kernel<T, D, E4M3, NT>), devices);
   if (e != cudaSuccess) return e;
   return launch_dependent(attend_kernel<T, D, E4M3, NT>, dim3((unsigned)grid), dim3(kThreads), Kernel<T, D, E4M3, NT>::smem, st, a);
 }
 template <typename T, int D>
-cudaError_t launch_d(const AttendArgs& a, bool e4m3, int nt, int grid, cudaStream_t st) {
+cudaError_t launch_d(const AttendArgs& a, bool e4m3, int nt, int sms, cudaStream_t st) {
   cudaError_t e;
-  if (e4m3) e = nt == 1 ? launch<T, D, true, 1>(a, grid, st) : launch<T, D, true, 2>(a, grid, st);
-  else e = nt == 1 ? launch<T, D, false, 1>(a, grid, st) : launch<T, D, false, 2>(a, grid, st);
+  int grid = 0;
+  if (e4m3) e = nt == 1 ? launch<T, D, true, 1>(a, sms, &grid, st) : launch<T, D, true, 2>(a, sms, &grid, st);
+  else e = nt == 1 ? launch<T, D, false, 1>(a, sms, &grid, st) : launch<T, D, false, 2>(a, sms, &grid, st);
   if (e != cudaSuccess) return e;
   return launch_dependent(join_kernel<T, D>, dim3((unsigned)grid, (unsigned)(8 * nt)), dim3(kThreads), 0, st, a);
 }
 template <typename T>
-cudaError_t launch_t(const AttendArgs& a, bool e4m3, int nt, int grid, cudaStream_t st) {
+cudaError_t launch_t(const AttendArgs& a, bool e4m3, int nt, int sms, cudaStream_t st) {
   switch (a.c.d) {
-    case 32: return launch_d<T, 32>(a, e4m3, nt, grid, st);
-    case 64: return launch_d<T, 64>(a, e4m3, nt, grid, st);
-    case 96: return launch_d<T, 96>(a, e4m3, nt, grid, st);
-    default: return launch_d<T, 128>(a, e4m3, nt, grid, st);
+    case 32: return launch_d<T, 32>(a, e4m3, nt, sms, st);
+    case 64: return launch_d<T, 64>(a, e4m3, nt, sms, st);
+    case 96: return launch_d<T, 96>(a, e4m3, nt, sms, st);
+    default: return launch_d<T, 128>(a, e4m3, nt, sms, st);
   }
 }
 
-constexpr int kCtasPerSm = 3;
+constexpr int kMostCtas = 3;   // per SM, of any instance
 
 struct Space {
   size_t meta, ml, o, bytes;
@@ -665,17 +720,17 @@ Space lay_out(int grid, int d) {
 
 }  // namespace
 
-size_t attend_space(int sms, int d) { return lay_out(sms * kCtasPerSm, d).bytes; }
+size_t attend_space(int sms, int d) { return lay_out(sms * kMostCtas, d).bytes; }
 
 cudaError_t launch_attend(AttendArgs& a, int dtype, bool e4m3, int cols, int sms, void* workspace, cudaStream_t st) {
-  const int grid = sms * kCtasPerSm;
+  const int grid = sms * kMostCtas;
   const Space s = lay_out(grid, a.c.d);
   char* w = static_cast<char*>(workspace);
   a.meta = reinterpret_cast<Meta*>(w + s.meta);
   a.part_ml = reinterpret_cast<float*>(w + s.ml);
   a.part_o = reinterpret_cast<float*>(w + s.o);
   const int nt = cols <= 8 ? 1 : 2;
-  return dtype == TQ_F32 ? launch_t<float>(a, e4m3, nt, grid, st) : launch_t<__nv_bfloat16>(a, e4m3, nt, grid, st);
+  return dtype == TQ_F32 ? launch_t<float>(a, e4m3, nt, sms, st) : launch_t<__nv_bfloat16>(a, e4m3, nt, sms, st);
 }
 
 }  // namespace kv8

@@ -52,10 +52,8 @@ __device__ __forceinline__ uint32_t half2_bits(float lo, float hi) {
 template <bool E4M3>
 __device__ __forceinline__ void expand(uint32_t w, uint32_t& lo, uint32_t& hi) {
   if (E4M3) {
-    const __half2_raw a = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w & 0xFFFFu), __NV_E4M3);
-    const __half2_raw b = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w >> 16), __NV_E4M3);
-    lo = (uint32_t)a.x | ((uint32_t)a.y << 16);
-    hi = (uint32_t)b.x | ((uint32_t)b.y << 16);
+    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}"
+        : "=r"(lo), "=r"(hi) : "r"(w));
   } else {
     w ^= 0x80808080u;
     const uint32_t a = __byte_perm(w, 0x64646464u, 0x4140), b = __byte_perm(w, 0x64646464u, 0x4342);
@@ -342,6 +340,10 @@ __global__ void __launch_bounds__(kThreads, Kernel<T, D, E4M3, NT>::kCtas) atten
     }
 
     // place s in the sequence, or in the listed pages one after another -> logical page, or -1
+    const int32_t* row_pages = a.b.table + (int64_t)b * a.b.ldt;   // not read where b < 0: such a row sees nothing
+    const int64_t head_bytes = (int64_t)D << a.c.page_shift, page_bytes = head_bytes * a.c.heads;
+    const uint8_t *k_head = a.c.k + head * head_bytes + 16 * lane, *v_head = a.c.v + head * head_bytes + 16 * lane;
+    const float* scales = (lane ? a.c.v_scale : a.c.k_scale) + head;
     const int i_first = (int)(u - item_at), i_stop = (int)(u_stop - item_at);   // of the item's units
     auto entry = [&](int i) -> int {
       if (i >= i_stop) return -1;
@@ -355,21 +357,24 @@ __global__ void __launch_bounds__(kThreads, Kernel<T, D, E4M3, NT>::kCtas) atten
       if (lp < 0) return r;
       const int64_t t0 = ((int64_t)lp << a.c.page_shift) + ((i * kUnit + warp * 16) & (T_ - 1));
       if (t0 >= vis_max) return r;
-      r.id = page_of(a.b, a.c.pages, b, lp);
-      r.t0 = r.id < 0 ? -1 : (int)t0;
+      const int id = row_pages[lp];       // a token that is seen lies inside the row's width
+      if (id < 0 || id >= a.c.pages) return r;
+      r.id = id;
+      r.t0 = (int)t0;
       return r;
     };
     uint8_t* ring = reinterpret_cast<uint8_t*>(smem4) + warp * K::kStages * K::kTile;
     auto issue = [&](const Group& g, int stage) {
       if (g.t0 >= 0) {
-        const int64_t blk = (int64_t)g.id * a.c.heads + head;
-        const int64_t at = ((blk << a.c.page_shift) + (g.t0 & (T_ - 1))) * D;
+        const int64_t at = g.id * page_bytes + (g.t0 & (T_ - 1)) * D;
         const uint32_t to = (uint32_t)__cvta_generic_to_shared(ring + stage * K::kTile);
 #pragma unroll
-        for (int x = lane; x < D; x += 32) copy16(to + 16 * key_chunk<D>(x / (D / 16), x % (D / 16)), a.c.k + at + 16 * x);
+        for (int i = 0; i < D / 32; ++i)
+          copy16(to + 16 * key_chunk<D>((lane + 32 * i) / (D / 16), (lane + 32 * i) % (D / 16)), k_head + at + 512 * i);
 #pragma unroll
-        for (int x = lane; x < D; x += 32) copy16(to + 16 * D + 16 * value_chunk<D>(x / (D / 16), x % (D / 16)), a.c.v + at + 16 * x);
-        if (lane < 2) copy4(to + 32 * D + 4 * lane, (lane ? a.c.v_scale : a.c.k_scale) + blk);
+        for (int i = 0; i < D / 32; ++i)
+          copy16(to + 16 * D + 16 * value_chunk<D>((lane + 32 * i) / (D / 16), (lane + 32 * i) % (D / 16)), v_head + at + 512 * i);
+        if (lane < 2) copy4(to + 32 * D + 4 * lane, scales + (int64_t)g.id * a.c.heads);
       }
       asm volatile("cp.async.commit_group;" ::: "memory");
     };

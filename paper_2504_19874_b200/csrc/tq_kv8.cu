@@ -360,14 +360,17 @@ __global__ void __launch_bounds__(kScoreWarps * 32) score_kernel(const __grid_co
   }
 }
 
-constexpr int kPickThreads = 512;
+constexpr int kPickThreads = 512, kPickWarps = kPickThreads / 32, kPickKeys = 8;
 
-// The k best keys of one (row, head) in ascending order of the page number, equal keys by the lower number: the k-th largest key by
-// four rounds of an 8-bit histogram, then one ordered pass that keeps what is above it and the first of its equals.
+// The k best keys of one (row, head) in ascending order of the page number, equal keys by the lower number.  Each round of an 8-bit
+// histogram narrows down the value of the last key that is taken, from the first bit in which the keys differ at all, and the rounds
+// end as soon as a whole bin is taken; then the pages are numbered through in order.  Up to 4,096 keys are held in registers (REG), more
+// are read again from L2.  Latency of a few barriers: one CTA per (row, head).
+template <bool REG>
 __global__ void __launch_bounds__(kPickThreads) pick_kernel(const __grid_constant__ SelectArgs a) {
-  __shared__ uint32_t hist[256];
-  __shared__ uint32_t prefix_s, need_s;
-  __shared__ uint32_t above_w[kPickThreads / 32], equal_w[kPickThreads / 32];
+  __shared__ uint32_t hist[2][256];
+  __shared__ uint32_t low_w[kPickWarps], high_w[kPickWarps], forced_w[kPickWarps];
+  __shared__ uint32_t above_w[kPickKeys * kPickWarps], equal_w[kPickKeys * kPickWarps];
   const int t = threadIdx.x, lane = t & 31, warp = t >> 5, h = blockIdx.x;
   const int64_t row = a.row0 + blockIdx.y;
   allow_successor();
@@ -383,71 +386,168 @@ __global__ void __launch_bounds__(kPickThreads) pick_kernel(const __grid_constan
     return;
   }
   const uint32_t* keys = a.keys + ((int64_t)blockIdx.y * a.c.heads + h) * a.b.width;
-  uint32_t prefix = 0u, need = (uint32_t)a.k;
+  uint32_t own[kPickKeys];
+  if (REG) {
 #pragma unroll
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    for (int i = t; i < 256; i += kPickThreads) hist[i] = 0u;
-    __syncthreads();
-    for (int i = t; i < count; i += kPickThreads) {
-      const uint32_t x = keys[i];
-      if (shift == 24 || (x >> (shift + 8)) == prefix) atomicAdd(&hist[(x >> shift) & 255u], 1u);
+    for (int j = 0; j < kPickKeys; ++j) own[j] = t + j * kPickThreads < count ? keys[t + j * kPickThreads] : 0u;
+  }
+  auto each = [&](auto&& f) {   // f(key, page) of this thread's pages
+    if (REG) {
+#pragma unroll
+      for (int j = 0; j < kPickKeys; ++j)
+        if (t + j * kPickThreads < count) f(own[j], t + j * kPickThreads);
+    } else {
+      for (int i = t; i < count; i += kPickThreads) f(keys[i], i);
     }
-    __syncthreads();
-    if (warp == 0) {   // lane l holds bins 255 - 8 l .. 248 - 8 l: the bin that the need-th largest key falls in
-      uint32_t own = 0u, bins[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        bins[i] = hist[255 - 8 * lane - i];
-        own += bins[i];
-      }
-      uint32_t upto = own;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const uint32_t y = __shfl_up_sync(0xffffffffu, upto, o);
-        if (lane >= o) upto += y;
-      }
-      uint32_t before = upto - own;
-      if (before < need && upto >= need) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          if (before < need && before + bins[i] >= need) {
-            prefix_s = (prefix << 8) | (uint32_t)(255 - 8 * lane - i);
-            need_s = need - before;
-            before = 0xFFFFFFFFu;
-          } else if (before != 0xFFFFFFFFu) {
-            before += bins[i];
-          }
-        }
-      }
+  };
+  // pages that are taken in any case have the largest key; the others' smallest and largest
+  uint32_t low = 0xFFFFFFFFu, high = 0u, forced = 0u;
+  each([&](uint32_t x, int) {
+    if (x == 0xFFFFFFFFu) {
+      ++forced;
+    } else {
+      low = min(low, x);
+      high = max(high, x);
     }
+  });
+  low = __reduce_min_sync(0xffffffffu, low);
+  high = __reduce_max_sync(0xffffffffu, high);
+  forced = __reduce_add_sync(0xffffffffu, forced);
+  if (lane == 0) {
+    low_w[warp] = low;
+    high_w[warp] = high;
+    forced_w[warp] = forced;
+  }
+  for (int i = t; i < 512; i += kPickThreads) hist[i >> 8][i & 255] = 0u;
+  __syncthreads();
+  low = __reduce_min_sync(0xffffffffu, low_w[lane % kPickWarps]);
+  high = __reduce_max_sync(0xffffffffu, high_w[lane % kPickWarps]);
+  forced = __reduce_add_sync(0xffffffffu, lane < kPickWarps ? forced_w[lane] : 0u);
+  uint32_t need = (uint32_t)a.k > forced ? (uint32_t)a.k - forced : 0u;   // of the others; there are more of them than that
+  // taken: keys above `edge`, and the first `need` of those equal to it
+  uint32_t edge = high;
+  int rest = low < high ? 32 - __clz(low ^ high) : 0;                     // bits in which keys may differ
+  uint32_t prefix = rest == 32 ? 0u : high >> rest;
+  bool whole = need == 0u;                                                // all keys at or above `edge` are taken
+  if (whole) edge = 0xFFFFFFFFu;
+  int round = 0;
+  while (rest > 0 && !whole) {
+    const int bits = min(rest, 8), shift = rest - bits;
+    uint32_t* hb = hist[round & 1];
+    each([&](uint32_t x, int) {
+      if (x != 0xFFFFFFFFu && (rest == 32 || (x >> rest) == prefix)) atomicAdd(&hb[(x >> shift) & ((1u << bits) - 1u)], 1u);
+    });
     __syncthreads();
-    prefix = prefix_s;
-    need = need_s;
+    // every warp looks for the bin that the need-th largest key falls into: lane l has bins 255 - 8 l .. 248 - 8 l
+    uint32_t bins[8], sum = 0u;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      bins[i] = hb[255 - 8 * lane - i];
+      sum += bins[i];
+    }
+    uint32_t upto = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t y = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += y;
+    }
+    uint32_t before = upto - sum, bin = 0u, left = 0u, size = 0u;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (before < need && before + bins[i] >= need) {
+        bin = 255u - 8u * lane - i;
+        left = need - before;
+        size = bins[i];
+      }
+      before += bins[i];
+    }
+    const int from = __ffs(__ballot_sync(0xffffffffu, size != 0u)) - 1;   // one lane has found it
+    bin = __shfl_sync(0xffffffffu, bin, from);
+    need = __shfl_sync(0xffffffffu, left, from);
+    size = __shfl_sync(0xffffffffu, size, from);
+    prefix = rest == 32 ? bin : (prefix << bits) | bin;
+    rest = shift;
+    edge = prefix << shift;
+    whole = need == size;
+    // the other histogram was last read before this round's barrier
+    for (int i = t; i < 256; i += kPickThreads) hist[(round + 1) & 1][i] = 0u;
+    ++round;
     __syncthreads();
   }
-  uint32_t above = 0u, equal = 0u;   // found before this chunk
-  for (int i0 = 0; i0 < count; i0 += kPickThreads) {
-    const int i = i0 + t;
-    const uint32_t x = i < count ? keys[i] : 0u;
-    const bool gt = i < count && x > prefix, eq = i < count && x == prefix;
-    const uint32_t bg = __ballot_sync(0xffffffffu, gt), be = __ballot_sync(0xffffffffu, eq);
-    if (lane == 0) {
-      above_w[warp] = __popc(bg);
-      equal_w[warp] = __popc(be);
-    }
-    __syncthreads();
-    uint32_t ga = above, ge = equal;
-    for (int w = 0; w < kPickThreads / 32; ++w) {
-      if (w == warp) {
-        const uint32_t my_g = ga + __popc(bg & ((1u << lane) - 1u)), my_e = ge + __popc(be & ((1u << lane) - 1u));
-        if (gt || (eq && my_e < need)) list[my_g + min(my_e, need)] = i;
+  if (whole) need = 0xFFFFFFFFu;
+  if (REG) {
+    uint32_t bg[kPickKeys], be[kPickKeys];
+#pragma unroll
+    for (int j = 0; j < kPickKeys; ++j) {
+      const bool in = t + j * kPickThreads < count;
+      bg[j] = __ballot_sync(0xffffffffu, in && own[j] > edge);
+      be[j] = __ballot_sync(0xffffffffu, in && own[j] == edge);
+      if (lane == 0) {
+        above_w[j * kPickWarps + warp] = __popc(bg[j]);
+        equal_w[j * kPickWarps + warp] = __popc(be[j]);
       }
-      ga += above_w[w];
-      ge += equal_w[w];
     }
-    above = ga;
-    equal = ge;
     __syncthreads();
+    if (warp == 0) {   // exclusive sums over the 128 (chunk, warp) counts, four per lane
+      uint32_t g[4], e[4], sg = 0u, se = 0u;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        g[i] = above_w[4 * lane + i];
+        e[i] = equal_w[4 * lane + i];
+        sg += g[i];
+        se += e[i];
+      }
+      uint32_t ug = sg, ue = se;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t yg = __shfl_up_sync(0xffffffffu, ug, o), ye = __shfl_up_sync(0xffffffffu, ue, o);
+        if (lane >= o) {
+          ug += yg;
+          ue += ye;
+        }
+      }
+      ug -= sg;
+      ue -= se;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        above_w[4 * lane + i] = ug;
+        equal_w[4 * lane + i] = ue;
+        ug += g[i];
+        ue += e[i];
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kPickKeys; ++j) {
+      const uint32_t under = (1u << lane) - 1u, g = above_w[j * kPickWarps + warp] + __popc(bg[j] & under),
+                     e = equal_w[j * kPickWarps + warp] + __popc(be[j] & under);
+      if (((bg[j] >> lane) & 1u) || (((be[j] >> lane) & 1u) && e < need)) list[g + min(e, need)] = t + j * kPickThreads;
+    }
+  } else {
+    uint32_t above = 0u, equal = 0u;   // found before this chunk
+    for (int i0 = 0; i0 < count; i0 += kPickThreads) {
+      const int i = i0 + t;
+      const uint32_t x = i < count ? keys[i] : 0u;
+      const bool gt = i < count && x > edge, eq = i < count && x == edge;
+      const uint32_t bg = __ballot_sync(0xffffffffu, gt), be = __ballot_sync(0xffffffffu, eq);
+      if (lane == 0) {
+        above_w[warp] = __popc(bg);
+        equal_w[warp] = __popc(be);
+      }
+      __syncthreads();
+      uint32_t ga = above, ge = equal;
+      for (int w = 0; w < kPickWarps; ++w) {
+        if (w == warp) {
+          const uint32_t g = ga + __popc(bg & ((1u << lane) - 1u)), e = ge + __popc(be & ((1u << lane) - 1u));
+          if (gt || (eq && e < need)) list[g + min(e, need)] = i;
+        }
+        ga += above_w[w];
+        ge += equal_w[w];
+      }
+      above = ga;
+      equal = ge;
+      __syncthreads();
+    }
   }
 }
 
@@ -564,7 +664,8 @@ extern "C" int tq_kv8_select(const tq_kv8* cache, const int32_t* table, int64_t 
       TQ_CHECK_CUDA(dtype == TQ_F32 ? launch_score<float>(a, grid, smem, st) : launch_score<__nv_bfloat16>(a, grid, smem, st), who);
       count_launches(1);
     }
-    TQ_CHECK_CUDA(launch_dependent(pick_kernel, dim3((unsigned)a.c.heads, (unsigned)rows), dim3(kPickThreads), 0, st, a), who);
+    TQ_CHECK_CUDA(launch_dependent(width <= kPickKeys * kPickThreads ? pick_kernel<true> : pick_kernel<false>,
+                                   dim3((unsigned)a.c.heads, (unsigned)rows), dim3(kPickThreads), 0, st, a), who);
     count_launches(1);
   }
   return TQ_OK;

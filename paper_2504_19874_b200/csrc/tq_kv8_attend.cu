@@ -99,6 +99,11 @@ __device__ __forceinline__ int value_chunk(int r, int x) {
   return r * (D / 16) + (D == 128 ? x ^ (r & 6) : (D == 64 ? x ^ (r & 2) : x));
 }
 
+// 64-bit divisions take hundreds of cycles, which the start of a short call would show; nearly all of these fit 32 bits.
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+  return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
+}
+
 // Units of sequence b (all heads and column blocks).  Sequences whose queries go to the many-query kernel have none here.
 struct Shape {
   int64_t begin, end, tokens;   // rows, cached tokens
@@ -110,7 +115,7 @@ __device__ __forceinline__ Shape shape_of(const AttendArgs& a, int b, int nc) {
   rows_of(a.b, b, &s.begin, &s.end);
   s.tokens = tokens_of(a.b, b, a.c.page_shift);
   const int64_t cols = (s.end - s.begin) * a.g;
-  s.blocks = cols > a.most_cols ? 0 : (int)((cols + nc - 1) / nc);
+  s.blocks = cols > a.most_cols ? 0 : (int)((cols + nc - 1) / nc);   // nc is a constant power of two
   s.units = s.blocks == 0 ? 0 : max((s.tokens + kUnit - 1) / kUnit, (int64_t)1);   // without tokens: one, for the zeros
   return s;
 }
@@ -199,7 +204,7 @@ __global__ void __launch_bounds__(kThreads, Kernel<T, D, E4M3, NT>::kCtas) atten
       }
       total += block_total(own, sums, &upto);
     }
-    per = max((total + gridDim.x - 1) / gridDim.x, (int64_t)1);
+    per = max(quotient(total + gridDim.x - 1, gridDim.x), (int64_t)1);
     const int64_t u0 = (int64_t)cta * per;
     if (u0 < total) {
       int64_t before = 0;
@@ -227,9 +232,9 @@ __global__ void __launch_bounds__(kThreads, Kernel<T, D, E4M3, NT>::kCtas) atten
       seq = found[0];
       const int64_t from = sums[6];
       sh = shape_of(a, seq, NC);
-      const int64_t i = (u0 - from) / sh.units;
-      head = (int)(i / sh.blocks);
-      block = (int)(i % sh.blocks);
+      const int64_t i = quotient(u0 - from, sh.units);
+      head = (int)i / sh.blocks;           // heads x blocks are below 2^31: 65535 heads, at most 2^15 blocks of the few columns here
+      block = (int)i % sh.blocks;
       item_at = from + i * sh.units;
     }
   } else {                               // rows x heads x blocks of columns, each of as many units as a list holds
@@ -241,11 +246,13 @@ __global__ void __launch_bounds__(kThreads, Kernel<T, D, E4M3, NT>::kCtas) atten
     sh.blocks = (a.g + NC - 1) / NC;
     list_units = max((((int64_t)a.nlist << a.c.page_shift) + kUnit - 1) / kUnit, (int64_t)1);
     total = rows * a.c.heads * sh.blocks * list_units;
-    per = max((total + gridDim.x - 1) / gridDim.x, (int64_t)1);
-    const int64_t i = (int64_t)cta * per / list_units;
-    seq = (int)(i / ((int64_t)a.c.heads * sh.blocks));          // a row here
-    head = (int)(i / sh.blocks % a.c.heads);
-    block = (int)(i % sh.blocks);
+    per = max(quotient(total + gridDim.x - 1, gridDim.x), (int64_t)1);
+    const int64_t i = quotient((int64_t)cta * per, list_units);
+    const int of_row = a.c.heads * sh.blocks;
+    seq = (int)quotient(i, of_row);                             // a row here
+    const int rest = (int)(i - (int64_t)seq * of_row);
+    head = rest / sh.blocks;
+    block = rest % sh.blocks;
     item_at = i * list_units;
   }
   int64_t u = (int64_t)cta * per;
@@ -278,33 +285,6 @@ __global__ void __launch_bounds__(kThreads, Kernel<T, D, E4M3, NT>::kCtas) atten
     }
     const int col0 = block * NC;
     const int64_t u_stop = min(u_end, item_at + units);
-    // ---- queries: scaled to [2^13, 2^14) per column, as fp16 limbs
-    for (int j = warp; j < NC; j += kWarps) {
-      const int jc = col0 + j;
-      const T* q = static_cast<const T*>(a.q) + (row0 + jc / width_c) * a.ldq + (int64_t)(head * a.g + jc % width_c) * a.hq;
-      float x[D / 32];
-      uint32_t most = 0u;
-#pragma unroll
-      for (int i = 0; i < D / 32; ++i) {
-        x[i] = j < cols ? (float)q[i * 32 + lane] : 0.f;
-        most = max(most, __float_as_uint(x[i]) & 0x7FFFFFFFu);
-      }
-      most = __reduce_max_sync(0xffffffffu, most);
-      // 2^e with e such that most * 2^-e is in [2^13, 2^14); 13 below the exponent of most, kept normal
-      const int e = min(max((int)(most >> 23) - 13, 1), 253);
-      const float s = __uint_as_float((uint32_t)e << 23), inv = __uint_as_float((uint32_t)(254 - e) << 23);
-#pragma unroll
-      for (int i = 0; i < D / 32; ++i) {
-        const float y = x[i] * inv;
-        const __half hi = __float2half_rn(y);
-        qsm[j * K::QP + i * 32 + lane] = hi;
-        if (LIMBS == 2) qsm[(NC + j) * K::QP + i * 32 + lane] = __float2half_rn(y - __half2float(hi));
-      }
-      // a row with an infinity or a NaN has no scores: NaN
-      if (lane == 0) fsm[j] = most >= 0x7F800000u ? __uint_as_float(0x7FC00000u) : s * (a.scale * kLog2e);
-    }
-    __syncthreads();
-    float f[NT][2];
     int vis[NT][2];                       // tokens that the column sees
     int vis_min = (int)min(tokens, (int64_t)INT32_MAX), vis_max = vis_min;
 #pragma unroll
@@ -312,23 +292,12 @@ __global__ void __launch_bounds__(kThreads, Kernel<T, D, E4M3, NT>::kCtas) atten
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const int j = nt * 8 + 2 * c4 + e;
-        f[nt][e] = fsm[j];
         vis[nt][e] = j < cols && a.lists == nullptr ? (int)max(tokens - (len_q - 1 - (col0 + j) / width_c), (int64_t)0) : vis_max;
       }
     if (a.lists == nullptr) {
       vis_min = (int)max(tokens - (len_q - 1 - col0 / width_c), (int64_t)0);
       vis_max = (int)max(tokens - (len_q - 1 - (col0 + cols - 1) / width_c), (int64_t)0);
     }
-    uint32_t qf[NT * LIMBS == 1 ? KW : 1][2];
-    if (NT * LIMBS == 1) {
-#pragma unroll
-      for (int w = 0; w < KW; ++w) {
-        const uint2 y = *reinterpret_cast<const uint2*>(qsm + n8 * K::QP + 4 * KS * 4 * (w / KS) + 4 * KS * c4 + 4 * (w % KS));
-        qf[w][0] = y.x;
-        qf[w][1] = y.y;
-      }
-    }
-
     float m[NT][2], l[NT][2], o[2 * VW][NT][4];
     float unit = 0.f, last_vs = 0.f, ratio = 0.f;
 #pragma unroll
@@ -378,6 +347,63 @@ __global__ void __launch_bounds__(kThreads, Kernel<T, D, E4M3, NT>::kCtas) atten
       }
       asm volatile("cp.async.commit_group;" ::: "memory");
     };
+    // the first steps are on their way while the queries are laid out
+    constexpr int S = K::kStages;
+    int t0s[S - 1];                      // first tokens of the steps in flight
+    int lps[S + 1];
+#pragma unroll
+    for (int i = 0; i < S + 1; ++i) lps[i] = entry(i_first + i);
+    Group gs[S];
+#pragma unroll
+    for (int i = 0; i < S; ++i) gs[i] = resolve(i_first + i, lps[i]);
+#pragma unroll
+    for (int i = 0; i < S - 1; ++i) {
+      issue(gs[i], i);
+      t0s[i] = gs[i].t0;
+    }
+    // ---- queries: scaled to [2^13, 2^14) per column, as fp16 limbs
+#pragma unroll
+    for (int ji = 0; ji < NC / kWarps; ++ji) {
+      const int j = ji * kWarps + warp;
+      const int jc = col0 + j;
+      const T* q = static_cast<const T*>(a.q) + (row0 + jc / width_c) * a.ldq + (int64_t)(head * a.g + jc % width_c) * a.hq;
+      float x[D / 32];
+      uint32_t most = 0u;
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i) {
+        x[i] = j < cols ? (float)q[i * 32 + lane] : 0.f;
+        most = max(most, __float_as_uint(x[i]) & 0x7FFFFFFFu);
+      }
+      most = __reduce_max_sync(0xffffffffu, most);
+      // 2^e with e such that most * 2^-e is in [2^13, 2^14); 13 below the exponent of most, kept normal
+      const int e = min(max((int)(most >> 23) - 13, 1), 253);
+      const float s = __uint_as_float((uint32_t)e << 23), inv = __uint_as_float((uint32_t)(254 - e) << 23);
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i) {
+        const float y = x[i] * inv;
+        const __half hi = __float2half_rn(y);
+        qsm[j * K::QP + i * 32 + lane] = hi;
+        if (LIMBS == 2) qsm[(NC + j) * K::QP + i * 32 + lane] = __float2half_rn(y - __half2float(hi));
+      }
+      // a row with an infinity or a NaN has no scores: NaN
+      if (lane == 0) fsm[j] = most >= 0x7F800000u ? __uint_as_float(0x7FC00000u) : s * (a.scale * kLog2e);
+    }
+    __syncthreads();
+    float f[NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) f[nt][e] = fsm[nt * 8 + 2 * c4 + e];
+    uint32_t qf[NT * LIMBS == 1 ? KW : 1][2];
+    if (NT * LIMBS == 1) {
+#pragma unroll
+      for (int w = 0; w < KW; ++w) {
+        const uint2 y = *reinterpret_cast<const uint2*>(qsm + n8 * K::QP + 4 * KS * 4 * (w / KS) + 4 * KS * c4 + 4 * (w % KS));
+        qf[w][0] = y.x;
+        qf[w][1] = y.y;
+      }
+    }
+
     auto compute = [&](int t0, int stage) {
       if (t0 < 0) return;
       const uint8_t* tile = ring + stage * K::kTile;
@@ -517,19 +543,6 @@ __global__ void __launch_bounds__(kThreads, Kernel<T, D, E4M3, NT>::kCtas) atten
       }
     };
     {
-      constexpr int S = K::kStages;
-      int t0s[S - 1];                      // first tokens of the steps in flight
-      int lps[S + 1];
-#pragma unroll
-      for (int i = 0; i < S + 1; ++i) lps[i] = entry(i_first + i);
-      Group gs[S];
-#pragma unroll
-      for (int i = 0; i < S; ++i) gs[i] = resolve(i_first + i, lps[i]);
-#pragma unroll
-      for (int i = 0; i < S - 1; ++i) {
-        issue(gs[i], i);
-        t0s[i] = gs[i].t0;
-      }
       Group next = gs[S - 1];
       int lp = lps[S], stage = 0;
       for (int i = i_first; i < i_stop; ++i) {
@@ -616,7 +629,7 @@ __global__ void __launch_bounds__(kThreads, Kernel<T, D, E4M3, NT>::kCtas) atten
       meta->col0 = col0;
       meta->cols = cols;
       meta->head = head;
-      meta->last_cta = (int)((item_at + units - 1) / per);
+      meta->last_cta = (int)quotient(item_at + units - 1, per);
     }
     __syncthreads();                       // shared memory is the next item's
     // ---- the next item
@@ -634,51 +647,73 @@ __global__ void __launch_bounds__(kThreads, Kernel<T, D, E4M3, NT>::kCtas) atten
   }
 }
 
-// Joins the parts of the item that began in CTA blockIdx.x's share, in the order of the shares.
+// Joins the parts of the item that began in CTA blockIdx.x's share, in the order of the shares: eight columns per blockIdx.y.  A warp
+// takes a column, or, where there are fewer than eight, an equal run of a column's parts, so that the loads of a long item (a head of
+// 32,768 tokens: 55 parts) are in flight together.
+constexpr int kJoinThreads = 256, kJoinParts = 64;
 template <typename T, int D>
-__global__ void __launch_bounds__(kThreads) join_kernel(const __grid_constant__ AttendArgs a) {
-  __shared__ float w_s[kThreads];
-  __shared__ float red_m[kWarps], red_l[kWarps];
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ AttendArgs a) {
+  __shared__ float w_s[8][kJoinParts];
+  __shared__ float4 o_s[8][32];
+  __shared__ float l_s[8];
   wait_for_predecessor();
   const Meta z = a.meta[blockIdx.x];
-  const int j = blockIdx.y, t = threadIdx.x, lane = t & 31, warp = t >> 5;
-  if (z.last_cta < 0 || j >= z.cols) return;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, j0 = 8 * blockIdx.y, cols = min(z.cols - j0, 8);
+  if (z.last_cta < 0 || cols <= 0) return;
   const int first = blockIdx.x, parts = z.last_cta - first + 1;
+  const int c2 = cols > 4 ? 8 : (cols > 2 ? 4 : cols), runs = 8 / c2, j = j0 + warp % c2, run = warp / c2;
+  const bool mine = j - j0 < cols;
   auto slot = [&](int i) { return 2 * (first + i) + (i == 0 ? 1 : 0); };
   float best = -TQ_INF;
-  for (int i = t; i < parts; i += kThreads) best = fmaxf(best, a.part_ml[(int64_t)slot(i) * 2 * kMaxCols + j]);
+  if (mine)
+    for (int i = lane; i < parts; i += 32) best = fmaxf(best, a.part_ml[(int64_t)slot(i) * 2 * kMaxCols + j]);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, o));
-  if (lane == 0) red_m[warp] = best;
-  __syncthreads();
-  best = fmaxf(fmaxf(red_m[0], red_m[1]), fmaxf(red_m[2], red_m[3]));
-  float sum = 0.f, y = 0.f;
-  for (int i0 = 0; i0 < parts; i0 += kThreads) {
-    const int n = min(parts - i0, kThreads);
-    float wl = 0.f;
-    __syncthreads();
-    if (t < n) {
-      const float* ml = a.part_ml + (int64_t)slot(i0 + t) * 2 * kMaxCols + j;
-      const float w = best == -TQ_INF ? 1.f : ex2(ml[0] - best);
-      w_s[t] = w;
-      wl = ml[kMaxCols] * w;
+  const int per = (parts + runs - 1) / runs, from = run * per, to = min(parts, from + per);
+  float sum = 0.f;
+  float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (mine)
+    for (int i0 = from; i0 < to; i0 += kJoinParts) {
+      const int n = min(to - i0, kJoinParts);
+      __syncwarp();
+      for (int i = lane; i < n; i += 32) {
+        const float* ml = a.part_ml + (int64_t)slot(i0 + i) * 2 * kMaxCols + j;
+        const float w = best == -TQ_INF ? 1.f : ex2(ml[0] - best);
+        w_s[warp][i] = w;
+        sum += ml[kMaxCols] * w;
+      }
+      __syncwarp();
+      if (lane < D / 4) {
+        const float* po = a.part_o + (int64_t)j * D + 4 * lane;
+#pragma unroll 8
+        for (int i = 0; i < n; ++i) {
+          const float4 v = *reinterpret_cast<const float4*>(po + (int64_t)slot(i0 + i) * kMaxCols * D);
+          const float w = w_s[warp][i];
+          y.x = fmaf(v.x, w, y.x); y.y = fmaf(v.y, w, y.y); y.z = fmaf(v.z, w, y.z); y.w = fmaf(v.w, w, y.w);
+        }
+      }
     }
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) wl += __shfl_xor_sync(0xffffffffu, wl, o);
-    if (lane == 0) red_l[warp] = wl;
-    __syncthreads();
-    sum += (red_l[0] + red_l[1]) + (red_l[2] + red_l[3]);
-    if (t < D) {
-      const float* po = a.part_o + (int64_t)j * D + t;
-#pragma unroll 8
-      for (int i = 0; i < n; ++i) y = fmaf(po[(int64_t)slot(i0 + i) * kMaxCols * D], w_s[i], y);
-    }
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  o_s[warp][lane] = y;
+  if (lane == 0) l_s[warp] = sum;
+  __syncthreads();
+  if (!mine || run != 0) return;
+  for (int r = 1; r < runs; ++r) {
+    const float4 v = o_s[warp + r * c2][lane];
+    y.x += v.x; y.y += v.y; y.z += v.z; y.w += v.w;
+    sum += l_s[warp + r * c2];
   }
   const int jc = z.col0 + j, g = a.g;
   const int64_t row = (int64_t)z.row0 + jc / g;
   const int head = z.head * g + jc % g;
-  if (t < D) store_out<T>(static_cast<T*>(a.out) + row * a.ldo + (int64_t)head * a.ho + t, sum == 0.f ? 0.f : y / sum);
-  if (t == 0 && a.lse) a.lse[row * ((int64_t)a.c.heads * g) + head] =
+  if (lane < D / 4) {
+    T* out = static_cast<T*>(a.out) + row * a.ldo + (int64_t)head * a.ho + 4 * lane;
+    const float v[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) store_out<T>(out + i, sum == 0.f ? 0.f : v[i] / sum);
+  }
+  if (lane == 0 && a.lse) a.lse[row * ((int64_t)a.c.heads * g) + head] =
       sum == 0.f ? -TQ_INF : (best == -TQ_INF ? 0.f : (best - kLift) * kLn2) + logf(sum);
 }
 
@@ -697,7 +732,7 @@ cudaError_t launch_d(const AttendArgs& a, bool e4m3, int nt, int sms, cudaStream
   if (e4m3) e = nt == 1 ? launch<T, D, true, 1>(a, sms, &grid, st) : launch<T, D, true, 2>(a, sms, &grid, st);
   else e = nt == 1 ? launch<T, D, false, 1>(a, sms, &grid, st) : launch<T, D, false, 2>(a, sms, &grid, st);
   if (e != cudaSuccess) return e;
-  return launch_dependent(join_kernel<T, D>, dim3((unsigned)grid, (unsigned)(8 * nt)), dim3(kThreads), 0, st, a);
+  return launch_dependent(join_kernel<T, D>, dim3((unsigned)grid, (unsigned)nt), dim3(kJoinThreads), 0, st, a);
 }
 template <typename T>
 cudaError_t launch_t(const AttendArgs& a, bool e4m3, int nt, int sms, cudaStream_t st) {

@@ -99,16 +99,11 @@ __device__ __forceinline__ int value_chunk(int r, int x) {
   return r * (D / 16) + (D == 128 ? x ^ (r & 6) : (D == 64 ? x ^ (r & 2) : x));
 }
 
-// 64-bit divisions take hundreds of cycles, which the start of a short call would show; nearly all of these fit 32 bits.
-__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
-  return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
-}
-
 // Units of sequence b (all heads and column blocks).  Sequences whose queries go to the many-query kernel have none here.
 struct Shape {
   int64_t begin, end, tokens;   // rows, cached tokens
   int blocks;                   // blocks of NC columns
-  int64_t units;                // of one (head, block)
+  int units;                    // of one (head, block); the host sees to it that all of a call's units fit 31 bits
 };
 __device__ __forceinline__ Shape shape_of(const AttendArgs& a, int b, int nc) {
   Shape s;
@@ -116,28 +111,28 @@ __device__ __forceinline__ Shape shape_of(const AttendArgs& a, int b, int nc) {
   s.tokens = tokens_of(a.b, b, a.c.page_shift);
   const int64_t cols = (s.end - s.begin) * a.g;
   s.blocks = cols > a.most_cols ? 0 : (int)((cols + nc - 1) / nc);   // nc is a constant power of two
-  s.units = s.blocks == 0 ? 0 : max((s.tokens + kUnit - 1) / kUnit, (int64_t)1);   // without tokens: one, for the zeros
+  s.units = s.blocks == 0 ? 0 : max((int)((s.tokens + kUnit - 1) / kUnit), 1);   // without tokens: one, for the zeros
   return s;
 }
 
-__device__ __forceinline__ int64_t block_total(int64_t v, int64_t* sums, int64_t* upto) {   // inclusive sum in order, and the total
+__device__ __forceinline__ int block_total(int v, int* sums, int* upto) {   // inclusive sum in order, and the total
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  int64_t s = v;
+  int x = v;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const int64_t y = __shfl_up_sync(0xffffffffu, s, o);
-    if (lane >= o) s += y;
+    const int y = __shfl_up_sync(0xffffffffu, x, o);
+    if (lane >= o) x += y;
   }
   __syncthreads();
-  if (lane == 31) sums[warp] = s;
+  if (lane == 31) sums[warp] = x;
   __syncthreads();
-  int64_t all = 0;
+  int all = 0;
 #pragma unroll
   for (int w = 0; w < kWarps; ++w) {
-    if (w < warp) s += sums[w];
+    if (w < warp) x += sums[w];
     all += sums[w];
   }
-  *upto = s;
+  *upto = x;
   return all;
 }
 
@@ -180,8 +175,7 @@ __global__ void __launch_bounds__(kThreads, Kernel<T, D, E4M3, NT>::kCtas) atten
   float* fsm = lsm + kWarps * NC;       // [NC] factor of a column's scores
   float* top = fsm + NC;                // [NC] maximum, then sum, of all warps
   float* tot = top + NC;
-  int64_t* sums = reinterpret_cast<int64_t*>(tot + NC);   // [8]
-  int* found = reinterpret_cast<int*>(sums + 8);
+  int* sums = reinterpret_cast<int*>(tot + NC);   // [8]
   const int t = threadIdx.x, lane = t & 31, warp = t >> 5, c4 = lane & 3, n8 = lane >> 2;
   const int cta = blockIdx.x;
   allow_successor();
@@ -189,52 +183,51 @@ __global__ void __launch_bounds__(kThreads, Kernel<T, D, E4M3, NT>::kCtas) atten
 
   // ---- this CTA's share [u, u_end) of all units, and the item that u falls into
   int seq = 0, head = 0, block = 0;
-  int64_t item_at = 0;                  // first unit of the item
-  int64_t total = 0, per;
+  int item_at = 0;                      // first unit of the item
+  int total = 0, per;
   Shape sh;
-  int64_t list_units = 0;
+  int list_units = 0;
   const int T_ = 1 << a.c.page_shift;
   if (a.lists == nullptr) {
-    int64_t upto = 0, own = 0;
+    int upto = 0, own = 0;
+    auto units_of = [&](int b) -> int {
+      if (b >= a.b.nseq) return 0;
+      const Shape s = shape_of(a, b, NC);
+      return s.units * s.blocks * a.c.heads;
+    };
+#pragma unroll 1
     for (int b0 = 0; b0 < a.b.nseq; b0 += kThreads) {
-      own = 0;
-      if (b0 + t < a.b.nseq) {
-        const Shape s = shape_of(a, b0 + t, NC);
-        own = s.units * s.blocks * a.c.heads;
-      }
+      own = units_of(b0 + t);
       total += block_total(own, sums, &upto);
     }
-    per = max(quotient(total + gridDim.x - 1, gridDim.x), (int64_t)1);
-    const int64_t u0 = (int64_t)cta * per;
+    per = max((total + (int)gridDim.x - 1) / (int)gridDim.x, 1);
+    const int u0 = cta * per;
     if (u0 < total) {
-      int64_t before = 0;
+      int before = 0;
+#pragma unroll 1
       for (int b0 = 0;; b0 += kThreads) {
-        int64_t all = total;
+        int all = total;
         if (a.b.nseq > kThreads) {
-          own = 0;
-          if (b0 + t < a.b.nseq) {
-            const Shape s = shape_of(a, b0 + t, NC);
-            own = s.units * s.blocks * a.c.heads;
-          }
+          own = units_of(b0 + t);
           all = block_total(own, sums, &upto);
         }
         if (before + all > u0) {
-          const int64_t from = before + upto - own;
-          if (own > 0 && from <= u0 && u0 < from + own) {
-            found[0] = b0 + t;
-            sums[6] = from;
+          const int from = before + upto - own;
+          if (from <= u0 && u0 < from + own) {
+            sums[4] = b0 + t;
+            sums[5] = from;
           }
           __syncthreads();
           break;
         }
         before += all;
       }
-      seq = found[0];
-      const int64_t from = sums[6];
+      seq = sums[4];
+      const int from = sums[5];
       sh = shape_of(a, seq, NC);
-      const int64_t i = quotient(u0 - from, sh.units);
-      head = (int)i / sh.blocks;           // heads x blocks are below 2^31: 65535 heads, at most 2^15 blocks of the few columns here
-      block = (int)i % sh.blocks;
+      const int i = (u0 - from) / sh.units;
+      head = i / sh.blocks;
+      block = i - head * sh.blocks;
       item_at = from + i * sh.units;
     }
   } else {                               // rows x heads x blocks of columns, each of as many units as a list holds
@@ -244,26 +237,26 @@ __global__ void __launch_bounds__(kThreads, Kernel<T, D, E4M3, NT>::kCtas) atten
       rows = rows < 0 ? 0 : (rows > a.b.n ? a.b.n : rows);
     }
     sh.blocks = (a.g + NC - 1) / NC;
-    list_units = max((((int64_t)a.nlist << a.c.page_shift) + kUnit - 1) / kUnit, (int64_t)1);
-    total = rows * a.c.heads * sh.blocks * list_units;
-    per = max(quotient(total + gridDim.x - 1, gridDim.x), (int64_t)1);
-    const int64_t i = quotient((int64_t)cta * per, list_units);
+    list_units = max((int)((((int64_t)a.nlist << a.c.page_shift) + kUnit - 1) / kUnit), 1);
     const int of_row = a.c.heads * sh.blocks;
-    seq = (int)quotient(i, of_row);                             // a row here
-    const int rest = (int)(i - (int64_t)seq * of_row);
-    head = rest / sh.blocks;
-    block = rest % sh.blocks;
+    total = (int)rows * of_row * list_units;
+    per = max((total + (int)gridDim.x - 1) / (int)gridDim.x, 1);
+    const int i = cta * per / list_units;
+    seq = i / of_row;                                           // a row here
+    head = (i - seq * of_row) / sh.blocks;
+    block = i - seq * of_row - head * sh.blocks;
     item_at = i * list_units;
   }
-  int64_t u = (int64_t)cta * per;
-  const int64_t u_end = min(total, u + per);
+  int u = cta * per;
+  const int u_end = min(total, u + per);
   Meta* meta = a.meta + cta;
   if (t == 0) meta->last_cta = -1;
   if (u >= u_end) return;
 
   while (u < u_end) {
     // ---- the item: rows, columns, what each column sees
-    int64_t row0, tokens, units;
+    int64_t row0, tokens;
+    int units;
     int b = seq, cols, width_c = a.g;    // columns of a row
     int64_t len_q;
     const int32_t* list = nullptr;
@@ -284,7 +277,7 @@ __global__ void __launch_bounds__(kThreads, Kernel<T, D, E4M3, NT>::kCtas) atten
       list = a.lists + (row0 * a.c.heads + head) * a.nlist;
     }
     const int col0 = block * NC;
-    const int64_t u_stop = min(u_end, item_at + units);
+    const int u_stop = min(u_end, item_at + units);
     int vis[NT][2];                       // tokens that the column sees
     int vis_min = (int)min(tokens, (int64_t)INT32_MAX), vis_max = vis_min;
 #pragma unroll
@@ -313,29 +306,37 @@ __global__ void __launch_bounds__(kThreads, Kernel<T, D, E4M3, NT>::kCtas) atten
     const int64_t head_bytes = (int64_t)D << a.c.page_shift, page_bytes = head_bytes * a.c.heads;
     const uint8_t *k_head = a.c.k + head * head_bytes + 16 * lane, *v_head = a.c.v + head * head_bytes + 16 * lane;
     const float* scales = (lane ? a.c.v_scale : a.c.k_scale) + head;
-    const int i_first = (int)(u - item_at), i_stop = (int)(u_stop - item_at);   // of the item's units
-    auto entry = [&](int i) -> int {
-      if (i >= i_stop) return -1;
-      const int lp = (int)(((int64_t)i * kUnit + warp * 16) >> a.c.page_shift);
-      if (list == nullptr) return lp;
-      return lp < a.nlist ? list[lp] : -1;
-    };
-    struct Group { int id, t0; };         // page and first token of 16 tokens; t0 < 0: nothing there
-    auto resolve = [&](int i, int lp) -> Group {
-      Group r{-1, -1};
-      if (lp < 0) return r;
-      const int64_t t0 = ((int64_t)lp << a.c.page_shift) + ((i * kUnit + warp * 16) & (T_ - 1));
-      if (t0 >= vis_max) return r;
-      const int id = row_pages[lp];       // a token that is seen lies inside the row's width
+    const int i_first = u - item_at, i_stop = u_stop - item_at;   // of the item's units
+    // Pages of 32 steps at a time, one per lane: what step i0 + lane reads.  `pos` is its first token, -1 where there is nothing.
+    struct Pages { int id, pos; };
+    auto look_up = [&](int i0) -> Pages {
+      Pages r{0, -1};
+      const int i = i0 + lane;
+      if (i >= i_stop) return r;
+      const int64_t s = (int64_t)i * kUnit + warp * 16;           // place in the sequence, or in the listed pages one after another
+      int64_t lp = s >> a.c.page_shift;
+      if (list != nullptr) lp = lp < a.nlist ? list[lp] : -1;
+      const int64_t t0 = (lp << a.c.page_shift) + (s & (T_ - 1));
+      if (lp < 0 || t0 >= vis_max) return r;
+      const int id = row_pages[lp];                               // a token that is seen lies inside the row's width
       if (id < 0 || id >= a.c.pages) return r;
       r.id = id;
-      r.t0 = (int)t0;
+      r.pos = (int)t0;
       return r;
     };
     uint8_t* ring = reinterpret_cast<uint8_t*>(smem4) + warp * K::kStages * K::kTile;
-    auto issue = [&](const Group& g, int stage) {
-      if (g.t0 >= 0) {
-        const int64_t at = g.id * page_bytes + (g.t0 & (T_ - 1)) * D;
+    Pages now = look_up(i_first), then = look_up(i_first + 32);
+    int base = i_first, to_issue = i_first;
+    auto issue = [&](int stage) {         // starts the copies of step `to_issue`; returns its first token
+      if (to_issue == base + 32) {
+        now = then;
+        base += 32;
+        then = look_up(base + 32);
+      }
+      const int id = __shfl_sync(0xffffffffu, now.id, to_issue - base), pos = __shfl_sync(0xffffffffu, now.pos, to_issue - base);
+      ++to_issue;
+      if (pos >= 0) {
+        const int64_t at = id * page_bytes + (pos & (T_ - 1)) * D;
         const uint32_t to = (uint32_t)__cvta_generic_to_shared(ring + stage * K::kTile);
 #pragma unroll
         for (int i = 0; i < D / 32; ++i)
@@ -343,24 +344,16 @@ __global__ void __launch_bounds__(kThreads, Kernel<T, D, E4M3, NT>::kCtas) atten
 #pragma unroll
         for (int i = 0; i < D / 32; ++i)
           copy16(to + 16 * D + 16 * value_chunk<D>((lane + 32 * i) / (D / 16), (lane + 32 * i) % (D / 16)), v_head + at + 512 * i);
-        if (lane < 2) copy4(to + 32 * D + 4 * lane, scales + (int64_t)g.id * a.c.heads);
+        if (lane < 2) copy4(to + 32 * D + 4 * lane, scales + (int64_t)id * a.c.heads);
       }
       asm volatile("cp.async.commit_group;" ::: "memory");
+      return pos;
     };
     // the first steps are on their way while the queries are laid out
     constexpr int S = K::kStages;
     int t0s[S - 1];                      // first tokens of the steps in flight
-    int lps[S + 1];
 #pragma unroll
-    for (int i = 0; i < S + 1; ++i) lps[i] = entry(i_first + i);
-    Group gs[S];
-#pragma unroll
-    for (int i = 0; i < S; ++i) gs[i] = resolve(i_first + i, lps[i]);
-#pragma unroll
-    for (int i = 0; i < S - 1; ++i) {
-      issue(gs[i], i);
-      t0s[i] = gs[i].t0;
-    }
+    for (int i = 0; i < S - 1; ++i) t0s[i] = issue(i);
     // ---- queries: scaled to [2^13, 2^14) per column, as fp16 limbs
 #pragma unroll
     for (int ji = 0; ji < NC / kWarps; ++ji) {
@@ -543,18 +536,15 @@ __global__ void __launch_bounds__(kThreads, Kernel<T, D, E4M3, NT>::kCtas) atten
       }
     };
     {
-      Group next = gs[S - 1];
-      int lp = lps[S], stage = 0;
+      int stage = 0;
+#pragma unroll 1
       for (int i = i_first; i < i_stop; ++i) {
         asm volatile("cp.async.wait_group %0;" ::"n"(S - 2) : "memory");
         __syncwarp();                      // the step's bytes are there for all lanes, and the last step's have been read
         const int t0 = t0s[0];
-        issue(next, stage == 0 ? S - 1 : stage - 1);
 #pragma unroll
         for (int j = 0; j < S - 2; ++j) t0s[j] = t0s[j + 1];
-        t0s[S - 2] = next.t0;
-        next = resolve(i + S, lp);
-        lp = entry(i + S + 1);
+        t0s[S - 2] = issue(stage == 0 ? S - 1 : stage - 1);
         compute(t0, stage);
         stage = stage == S - 1 ? 0 : stage + 1;
       }
@@ -629,7 +619,7 @@ __global__ void __launch_bounds__(kThreads, Kernel<T, D, E4M3, NT>::kCtas) atten
       meta->col0 = col0;
       meta->cols = cols;
       meta->head = head;
-      meta->last_cta = (int)quotient(item_at + units - 1, per);
+      meta->last_cta = (item_at + units - 1) / per;
     }
     __syncthreads();                       // shared memory is the next item's
     // ---- the next item
@@ -648,20 +638,19 @@ __global__ void __launch_bounds__(kThreads, Kernel<T, D, E4M3, NT>::kCtas) atten
 }
 
 // Joins the parts of the item that began in CTA blockIdx.x's share, in the order of the shares: eight columns per blockIdx.y.  A warp
-// takes a column, or, where there are fewer than eight, an equal run of a column's parts, so that the loads of a long item (a head of
-// 32,768 tokens: 55 parts) are in flight together.
-constexpr int kJoinThreads = 256, kJoinParts = 64;
+// takes an equal run of a column's parts, so that the loads of a long item (a head of 32,768 tokens: 52 parts) are in flight together.
+constexpr int kJoinThreads = 512, kJoinWarps = kJoinThreads / 32, kJoinParts = 32;
 template <typename T, int D>
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ AttendArgs a) {
-  __shared__ float w_s[8][kJoinParts];
-  __shared__ float4 o_s[8][32];
-  __shared__ float l_s[8];
+  __shared__ float w_s[kJoinWarps][kJoinParts];
+  __shared__ float4 o_s[kJoinWarps][32];
+  __shared__ float l_s[kJoinWarps];
   wait_for_predecessor();
   const Meta z = a.meta[blockIdx.x];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, j0 = 8 * blockIdx.y, cols = min(z.cols - j0, 8);
   if (z.last_cta < 0 || cols <= 0) return;
   const int first = blockIdx.x, parts = z.last_cta - first + 1;
-  const int c2 = cols > 4 ? 8 : (cols > 2 ? 4 : cols), runs = 8 / c2, j = j0 + warp % c2, run = warp / c2;
+  const int c2 = cols > 4 ? 8 : (cols > 2 ? 4 : cols), runs = kJoinWarps / c2, j = j0 + warp % c2, run = warp / c2;
   const bool mine = j - j0 < cols;
   auto slot = [&](int i) { return 2 * (first + i) + (i == 0 ? 1 : 0); };
   float best = -TQ_INF;
@@ -676,7 +665,7 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
     for (int i0 = from; i0 < to; i0 += kJoinParts) {
       const int n = min(to - i0, kJoinParts);
       __syncwarp();
-      for (int i = lane; i < n; i += 32) {
+      for (int i = lane; i < n; i += 32) {   // once: kJoinParts is a warp
         const float* ml = a.part_ml + (int64_t)slot(i0 + i) * 2 * kMaxCols + j;
         const float w = best == -TQ_INF ? 1.f : ex2(ml[0] - best);
         w_s[warp][i] = w;
@@ -813,6 +802,10 @@ extern "C" int tq_kv8_attend(const tq_kv8* cache, const int32_t* table, int64_t 
   const size_t need = tq_kv8_attend_workspace_bytes(cache, nseq, n, q_per_kv, max_queries, nlist);
   TQ_REQUIRE(workspace != nullptr && workspace_bytes >= need, TQ_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", who, workspace_bytes, need);
   TQ_REQUIRE((reinterpret_cast<uintptr_t>(workspace) & 255) == 0, TQ_ERR_ALIGNMENT, "%s: workspace is not 256-byte aligned", who);
+  // units of 64 tokens, over all heads and blocks of eight columns, are numbered in 31 bits
+  const double units = (lists ? (double)n * (((double)nlist * cache->page_tokens + 63) / 64 + 1) * ((q_per_kv + 7) / 8)
+                              : (double)nseq * (((double)width * cache->page_tokens + 63) / 64 + 1) * 2) * cache->heads;
+  TQ_REQUIRE(units < 2.0e9, TQ_ERR_UNSUPPORTED, "%s: %.3g units of 64 tokens in one call", who, units);
   int dev = 0, sms = 0;
   TQ_CHECK_CUDA(cudaGetDevice(&dev), who);
   TQ_CHECK_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev), who);

@@ -25,15 +25,6 @@ namespace {
 
 constexpr int kWarps = 4, kThreads = kWarps * 32;
 constexpr int kUnit = 64;                // tokens
-constexpr float kLift = 6.f, kSlack = 8.f;
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-#define TQ_INF __uint_as_float(0x7F800000u)
-
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 __device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
@@ -155,13 +146,6 @@ struct Kernel {
   static constexpr size_t head = ring > o_bytes ? ring : o_bytes;   // the results take the ring's place
   static constexpr size_t smem = head + q_bytes + sizeof(float) * (2 * kWarps + 3) * NC + 256;
 };
-
-template <typename T>
-__device__ __forceinline__ void store_out(T* p, float x);
-template <>
-__device__ __forceinline__ void store_out<float>(float* p, float x) { *p = x; }
-template <>
-__device__ __forceinline__ void store_out<__nv_bfloat16>(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
 
 template <typename T, int D, bool E4M3, int NT>
 __global__ void __launch_bounds__(kThreads, Kernel<T, D, E4M3, NT>::kCtas) attend_kernel(const __grid_constant__ AttendArgs a) {
@@ -325,6 +309,15 @@ __global__ void __launch_bounds__(kThreads, Kernel<T, D, E4M3, NT>::kCtas) atten
       return r;
     };
     uint8_t* ring = reinterpret_cast<uint8_t*>(smem4) + warp * K::kStages * K::kTile;
+    // the queries are read before the first steps' copies queue up, and laid out while those are on their way
+    float qx[NC / kWarps][D / 32];
+#pragma unroll
+    for (int ji = 0; ji < NC / kWarps; ++ji) {
+      const int jc = col0 + ji * kWarps + warp;
+      const T* q = static_cast<const T*>(a.q) + (row0 + jc / width_c) * a.ldq + (int64_t)(head * a.g + jc % width_c) * a.hq;
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i) qx[ji][i] = ji * kWarps + warp < cols ? (float)q[i * 32 + lane] : 0.f;
+    }
     Pages now = look_up(i_first), then = look_up(i_first + 32);
     int base = i_first, to_issue = i_first;
     auto issue = [&](int stage) {         // starts the copies of step `to_issue`; returns its first token
@@ -349,7 +342,6 @@ __global__ void __launch_bounds__(kThreads, Kernel<T, D, E4M3, NT>::kCtas) atten
       asm volatile("cp.async.commit_group;" ::: "memory");
       return pos;
     };
-    // the first steps are on their way while the queries are laid out
     constexpr int S = K::kStages;
     int t0s[S - 1];                      // first tokens of the steps in flight
 #pragma unroll
@@ -358,19 +350,13 @@ __global__ void __launch_bounds__(kThreads, Kernel<T, D, E4M3, NT>::kCtas) atten
 #pragma unroll
     for (int ji = 0; ji < NC / kWarps; ++ji) {
       const int j = ji * kWarps + warp;
-      const int jc = col0 + j;
-      const T* q = static_cast<const T*>(a.q) + (row0 + jc / width_c) * a.ldq + (int64_t)(head * a.g + jc % width_c) * a.hq;
-      float x[D / 32];
+      const float (&x)[D / 32] = qx[ji];
       uint32_t most = 0u;
 #pragma unroll
-      for (int i = 0; i < D / 32; ++i) {
-        x[i] = j < cols ? (float)q[i * 32 + lane] : 0.f;
-        most = max(most, __float_as_uint(x[i]) & 0x7FFFFFFFu);
-      }
+      for (int i = 0; i < D / 32; ++i) most = max(most, __float_as_uint(x[i]) & 0x7FFFFFFFu);
       most = __reduce_max_sync(0xffffffffu, most);
-      // 2^e with e such that most * 2^-e is in [2^13, 2^14); 13 below the exponent of most, kept normal
-      const int e = min(max((int)(most >> 23) - 13, 1), 253);
-      const float s = __uint_as_float((uint32_t)e << 23), inv = __uint_as_float((uint32_t)(254 - e) << 23);
+      float inv;
+      const float s = query_scale(most, &inv);
 #pragma unroll
       for (int i = 0; i < D / 32; ++i) {
         const float y = x[i] * inv;
@@ -639,10 +625,9 @@ __global__ void __launch_bounds__(kThreads, Kernel<T, D, E4M3, NT>::kCtas) atten
 
 // Joins the parts of the item that began in CTA blockIdx.x's share, in the order of the shares: eight columns per blockIdx.y.  A warp
 // takes an equal run of a column's parts, so that the loads of a long item (a head of 32,768 tokens: 52 parts) are in flight together.
-constexpr int kJoinThreads = 512, kJoinWarps = kJoinThreads / 32, kJoinParts = 32;
+constexpr int kJoinThreads = 512, kJoinWarps = kJoinThreads / 32, kJoinParts = 8;
 template <typename T, int D>
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ AttendArgs a) {
-  __shared__ float w_s[kJoinWarps][kJoinParts];
   __shared__ float4 o_s[kJoinWarps][32];
   __shared__ float l_s[kJoinWarps];
   wait_for_predecessor();
@@ -655,33 +640,34 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
   auto slot = [&](int i) { return 2 * (first + i) + (i == 0 ? 1 : 0); };
   float best = -TQ_INF;
   if (mine)
-    for (int i = lane; i < parts; i += 32) best = fmaxf(best, a.part_ml[(int64_t)slot(i) * 2 * kMaxCols + j]);
+    for (int i = lane; i < parts; i += 32) best = fmaxf(best, a.part_ml[(int64_t)slot(i) * 2 * a.pitch + j]);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, o));
   const int per = (parts + runs - 1) / runs, from = run * per, to = min(parts, from + per);
   float sum = 0.f;
   float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (mine)
+  if (mine) {
+    const float* po = a.part_o + (int64_t)j * D + 4 * min(lane, D / 4 - 1);
+#pragma unroll 1
     for (int i0 = from; i0 < to; i0 += kJoinParts) {
-      const int n = min(to - i0, kJoinParts);
-      __syncwarp();
-      for (int i = lane; i < n; i += 32) {   // once: kJoinParts is a warp
-        const float* ml = a.part_ml + (int64_t)slot(i0 + i) * 2 * kMaxCols + j;
-        const float w = best == -TQ_INF ? 1.f : ex2(ml[0] - best);
-        w_s[warp][i] = w;
-        sum += ml[kMaxCols] * w;
+      float4 v[kJoinParts];              // their loads wait for no weight; places behind the last part are read again, with weight 0
+#pragma unroll
+      for (int i = 0; i < kJoinParts; ++i) v[i] = *reinterpret_cast<const float4*>(po + (int64_t)slot(min(i0 + i, to - 1)) * a.pitch * D);
+      float w = 0.f;
+      if (lane < kJoinParts && i0 + lane < to) {
+        const float* ml = a.part_ml + (int64_t)slot(i0 + lane) * 2 * a.pitch + j;
+        w = best == -TQ_INF ? 1.f : ex2(ml[0] - best);
+        sum += ml[a.pitch] * w;
       }
-      __syncwarp();
-      if (lane < D / 4) {
-        const float* po = a.part_o + (int64_t)j * D + 4 * lane;
-#pragma unroll 8
-        for (int i = 0; i < n; ++i) {
-          const float4 v = *reinterpret_cast<const float4*>(po + (int64_t)slot(i0 + i) * kMaxCols * D);
-          const float w = w_s[warp][i];
-          y.x = fmaf(v.x, w, y.x); y.y = fmaf(v.y, w, y.y); y.z = fmaf(v.z, w, y.z); y.w = fmaf(v.w, w, y.w);
+#pragma unroll
+      for (int i = 0; i < kJoinParts; ++i) {
+        const float wi = __shfl_sync(0xffffffffu, w, i);
+        if (i0 + i < to) {               // a part without tokens may hold what is not a number
+          y.x = fmaf(v[i].x, wi, y.x); y.y = fmaf(v[i].y, wi, y.y); y.z = fmaf(v[i].z, wi, y.z); y.w = fmaf(v[i].w, wi, y.w);
         }
       }
     }
+  }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
   o_s[warp][lane] = y;
@@ -721,7 +707,7 @@ cudaError_t launch_d(const AttendArgs& a, bool e4m3, int nt, int sms, cudaStream
   if (e4m3) e = nt == 1 ? launch<T, D, true, 1>(a, sms, &grid, st) : launch<T, D, true, 2>(a, sms, &grid, st);
   else e = nt == 1 ? launch<T, D, false, 1>(a, sms, &grid, st) : launch<T, D, false, 2>(a, sms, &grid, st);
   if (e != cudaSuccess) return e;
-  return launch_dependent(join_kernel<T, D>, dim3((unsigned)grid, (unsigned)nt), dim3(kJoinThreads), 0, st, a);
+  return launch_join(a, sizeof(T) == 4 ? TQ_F32 : TQ_BF16, grid, nt, st);
 }
 template <typename T>
 cudaError_t launch_t(const AttendArgs& a, bool e4m3, int nt, int sms, cudaStream_t st) {
@@ -749,6 +735,20 @@ Space lay_out(int grid, int d) {
 
 }  // namespace
 
+template <typename T>
+static cudaError_t join_t(const AttendArgs& a, dim3 grid, cudaStream_t st) {
+  switch (a.c.d) {
+    case 32: return launch_dependent(join_kernel<T, 32>, grid, dim3(kJoinThreads), 0, st, a);
+    case 64: return launch_dependent(join_kernel<T, 64>, grid, dim3(kJoinThreads), 0, st, a);
+    case 96: return launch_dependent(join_kernel<T, 96>, grid, dim3(kJoinThreads), 0, st, a);
+    default: return launch_dependent(join_kernel<T, 128>, grid, dim3(kJoinThreads), 0, st, a);
+  }
+}
+cudaError_t launch_join(const AttendArgs& a, int dtype, int grid, int blocks, cudaStream_t st) {
+  const dim3 g((unsigned)grid, (unsigned)blocks);
+  return dtype == TQ_F32 ? join_t<float>(a, g, st) : join_t<__nv_bfloat16>(a, g, st);
+}
+
 size_t attend_space(int sms, int d) { return lay_out(sms * kMostCtas, d).bytes; }
 
 cudaError_t launch_attend(AttendArgs& a, int dtype, bool e4m3, int cols, int sms, void* workspace, cudaStream_t st) {
@@ -758,6 +758,7 @@ cudaError_t launch_attend(AttendArgs& a, int dtype, bool e4m3, int cols, int sms
   a.meta = reinterpret_cast<Meta*>(w + s.meta);
   a.part_ml = reinterpret_cast<float*>(w + s.ml);
   a.part_o = reinterpret_cast<float*>(w + s.o);
+  a.pitch = kMaxCols;
   const int nt = cols <= 8 ? 1 : 2;
   return dtype == TQ_F32 ? launch_t<float>(a, e4m3, nt, sms, st) : launch_t<__nv_bfloat16>(a, e4m3, nt, sms, st);
 }
@@ -770,8 +771,9 @@ extern "C" size_t tq_kv8_attend_workspace_bytes(const tq_kv8* cache, int nseq, i
   using namespace tq::kv8;
   int dev = 0, sms = 0;
   if (cache == nullptr || cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
-  (void)nseq; (void)n; (void)q_per_kv; (void)max_queries; (void)nlist;
-  return attend_space(sms, cache->d);
+  (void)nseq; (void)n;
+  const bool many = nlist == 0 && (int64_t)max_queries * q_per_kv > kMaxCols;
+  return attend_space(sms, cache->d) + (many ? prompt_space(sms, cache->d) : 0);
 }
 
 extern "C" int tq_kv8_attend(const tq_kv8* cache, const int32_t* table, int64_t ldt, int width, int nseq, const int32_t* tokens,
@@ -804,16 +806,26 @@ extern "C" int tq_kv8_attend(const tq_kv8* cache, const int32_t* table, int64_t 
   TQ_REQUIRE((reinterpret_cast<uintptr_t>(workspace) & 255) == 0, TQ_ERR_ALIGNMENT, "%s: workspace is not 256-byte aligned", who);
   // units of 64 tokens, over all heads and blocks of eight columns, are numbered in 31 bits
   const double units = (lists ? (double)n * (((double)nlist * cache->page_tokens + 63) / 64 + 1) * ((q_per_kv + 7) / 8)
-                              : (double)nseq * (((double)width * cache->page_tokens + 63) / 64 + 1) * 2) * cache->heads;
-  TQ_REQUIRE(units < 2.0e9, TQ_ERR_UNSUPPORTED, "%s: %.3g units of 64 tokens in one call", who, units);
+                              : ((double)nseq * 2 + (double)n * q_per_kv / 128) * (((double)width * cache->page_tokens + 63) / 64 + 1)) * cache->heads;
+  TQ_REQUIRE(units < 2.0e9 && (double)n * q_per_kv < 2.0e9, TQ_ERR_UNSUPPORTED, "%s: %.3g units of 64 tokens in one call", who, units);
   int dev = 0, sms = 0;
   TQ_CHECK_CUDA(cudaGetDevice(&dev), who);
   TQ_CHECK_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev), who);
   a.q = Q; a.ldq = ldq; a.hq = hq; a.g = q_per_kv; a.scale = scale;
   a.lists = lists; a.nlist = nlist; a.out = out; a.ldo = ldo; a.ho = ho; a.lse = lse;
-  a.most_cols = INT32_MAX;
+  // Sequences with up to 16 columns (rows x heads of a group) are bound by the cache's bytes and go to the few-query kernel, the others
+  // to the many-query one; a batch of both kinds runs both, each over its own.
   const int64_t cols = lists ? q_per_kv : (int64_t)max_queries * q_per_kv;
-  TQ_CHECK_CUDA(launch_attend(a, dtype, cache->code_type == TQ_E4M3, (int)std::min<int64_t>(cols, 16), sms, workspace, static_cast<cudaStream_t>(stream)), who);
-  count_launches(2);
+  const bool e4m3 = cache->code_type == TQ_E4M3, many = lists == nullptr && cols > kMaxCols;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  a.most_cols = many && nseq == 1 ? 0 : kMaxCols;   // a single sequence goes to one kernel, however many rows it turns out to have
+  if (many) {
+    TQ_CHECK_CUDA(launch_prompt(a, dtype, e4m3, sms, static_cast<char*>(workspace) + attend_space(sms, a.c.d), st), who);
+    count_launches(2);
+  }
+  if (!many || nseq > 1) {
+    TQ_CHECK_CUDA(launch_attend(a, dtype, e4m3, (int)std::min<int64_t>(cols, kMaxCols), sms, workspace, st), who);
+    count_launches(2);
+  }
   return TQ_OK;
 }

@@ -1,0 +1,744 @@
+// Attention over a paged 8-bit KV cache for many queries per sequence (prompts, chunks of prompts), on tcgen05.
+//
+// Mathematics.  Rows are (token, head of the group) pairs of one sequence and KV head; per tile of 128 rows and 128 keys
+//   S = Q K^T (TMEM),  p = 2^(s - m + 6) with the row's running maximum m,  O += P V (TMEM, P as the A operand from TMEM).
+// As in the few-query kernel queries are scaled per row by a power of two into [2^13, 2^14) and held in fp16 (fp32 ones as two limbs),
+// P is one fp16 limb for bf16 outputs and two for fp32 ones, and m moves only when a score exceeds it by 2^8: then the row's O in
+// TMEM is rescaled by its own thread.  All sums are fp32.
+// The codes become fp16 in shared memory, times their block's scale over the largest scale of the pages in hand (a power of two, so
+// exact down to 2^-24 of that scale, 2^-31 of the largest number): the one factor left per row goes into the softmax or the output.
+//
+// Work.  A CTA per SM; units are (tile of 128 keys) x (block of 256 rows, fp32: 128), numbered through over blocks, heads and sequences,
+// and every CTA takes an equal run of them, so that causal triangles and ragged batches are even; runs that end inside a block leave
+// parts that the join kernel adds up.
+// Warps: two groups of four for the softmax of a row tile each (a thread per row, no shuffles), three that expand codes from global memory
+// through registers into the operand layout, one that issues the MMAs.  While one group works on its S, the tensor cores work for the
+// other.  Waits are bounded; a CTA that gives up writes NaN.
+#include <algorithm>
+#include <cstring>
+
+#include "tq_kv8.h"
+#include "tq_kv8_attend.h"
+#include "tq_tc.cuh"
+
+namespace tq {
+namespace kv8 {
+namespace {
+
+constexpr int kExpandWarps = 3, kThreads = 384, kExpandWarp0 = 8, kMmaWarp = 11;   // three warps per scheduler: 168 registers each
+constexpr int kKeys = 128;                  // of a tile
+constexpr uint32_t kPanel = kKeys * 128;    // bytes of 128 rows x 64 fp16
+
+template <typename T, int D>
+struct Shape {
+  static constexpr int kLimbs = sizeof(T) == 4 ? 2 : 1;
+  static constexpr int kTiles = kLimbs == 2 ? 1 : 2;
+  static constexpr int kRows = 128 * kTiles;
+  static constexpr int kPanels = (D + 63) / 64;
+  static constexpr uint32_t kOperand = kPanels * kPanel;          // a tile of 128 rows: queries, keys or values
+  static constexpr uint32_t smem = 6 * kOperand + 1024 + 1024;    // two of queries (row tiles, or limbs), two stages of keys and values
+};
+
+struct Bars {
+  uint64_t q_ready, o_done, drain, k_full[2], k_empty[2], v_full[2], v_empty[2], s_ready[2], p_ready[2];
+};
+struct Shared {
+  Bars bar;
+  float uk[4], uv[4];                       // largest scales of the items in hand, by the item's number
+  int flags[4];                             // of tiles, by number: bits 0-7: 16 keys whose values are NaN; 8-15: 16 keys of no page
+  uint32_t tmem;
+  int abort_flag;
+  int sums[16], found[4];
+};
+
+// ---- work: full blocks of `rows` rows of a sequence see ever more keys; the sum over the first n of them in closed form
+__device__ __forceinline__ int64_t quot(int64_t a, int64_t b) {
+  return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
+}
+// sum over 0 <= i < n of floor((a i + b) / m), for non-negative a, b
+__device__ __noinline__ int64_t floor_sum(int64_t n, int64_t m, int64_t a, int64_t b) {
+  int64_t s = 0;
+  while (true) {
+    if (a >= m) {
+      const int64_t q = quot(a, m);
+      s += n * (n - 1) / 2 * q;
+      a -= q * m;
+    }
+    if (b >= m) {
+      const int64_t q = quot(b, m);
+      s += n * q;
+      b -= q * m;
+    }
+    const int64_t top = a * n + b;
+    if (top < m) return s;
+    n = quot(top, m);
+    b = top - n * m;
+    const int64_t t = m;
+    m = a;
+    a = t;
+  }
+}
+struct Seq {              // the host sees to it that columns and units fit 31 bits
+  int begin, len_q, tokens, blocks;
+};
+__device__ __forceinline__ Seq seq_of(const AttendArgs& a, int b, int rows) {
+  Seq s;
+  int64_t begin, end;
+  rows_of(a.b, b, &begin, &end);
+  s.begin = (int)begin;
+  s.len_q = (int)(end - begin);
+  s.tokens = (int)min(tokens_of(a.b, b, a.c.page_shift), (int64_t)INT32_MAX);
+  const int cols = s.len_q * a.g;
+  s.blocks = cols > a.most_cols ? (cols + rows - 1) / rows : 0;
+  return s;
+}
+// Keys that row c of the sequence's columns sees.
+__device__ __forceinline__ int seen_by(const AttendArgs& a, const Seq& s, int c) { return max(s.tokens - (s.len_q - 1 - c / a.g), 0); }
+// Key tiles of the first n blocks.
+__device__ __forceinline__ int tiles_before(const AttendArgs& a, const Seq& s, int rows, int n) {
+  if (n <= 0) return 0;
+  int sum = 0;
+  if (n == s.blocks) {   // the last block may be short: it sees all keys
+    sum = max((int)(((int64_t)s.tokens + kKeys - 1) / kKeys), 1);
+    --n;
+  }
+  // block k sees vis = c + floor((rows k + rows - 1) / g) keys, c = tokens - len_q + 1, and has max(1, ceil(vis / 128)) tiles
+  const int64_t c = (int64_t)s.tokens - s.len_q + 1, m = (int64_t)kKeys * a.g;
+  int64_t b = rows - 1 + a.g * (c + kKeys - 1);
+  int k0 = 0;
+  if (b < m) {           // the first blocks have fewer than one: they count as one
+    k0 = (int)min((int64_t)n, quot(m - b + rows - 1, rows));
+    sum += k0;
+    b += (int64_t)k0 * rows;
+  }
+  if (n > k0) sum += (int)floor_sum(n - k0, m, rows, b);
+  return sum;
+}
+
+struct Item {
+  int b, head, block;
+  int row0, col0;        // first row of Q, first column of the block
+  int cols, tiles;       // its columns, its key tiles
+  int vis_min, vis_max;  // keys that its first and its last column see
+  Seq s;
+};
+__device__ __forceinline__ void describe(const AttendArgs& a, int rows, Item* it) {
+  it->row0 = it->s.begin;
+  it->col0 = it->block * rows;
+  it->cols = min(it->s.len_q * a.g - it->col0, rows);
+  it->vis_min = seen_by(a, it->s, it->col0);
+  it->vis_max = seen_by(a, it->s, it->col0 + it->cols - 1);
+  it->tiles = max((int)(((int64_t)it->vis_max + kKeys - 1) / kKeys), 1);
+}
+__device__ __forceinline__ void next_item(const AttendArgs& a, int rows, Item* it) {   // the caller knows that there is one
+  if (++it->block == it->s.blocks) {
+    it->block = 0;
+    if (++it->head == a.c.heads) {
+      it->head = 0;
+      do it->s = seq_of(a, ++it->b, rows);
+      while (it->s.blocks == 0);
+    }
+  }
+  describe(a, rows, it);
+}
+
+// ---- tcgen05 forms that the other kernels do not use
+// D (+)= A[tmem] B[smem], fp16 operands.
+__device__ __forceinline__ void umma_f16_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+      ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+      ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
+        "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
+      : "memory");
+}
+// Values as the B operand with n (channels) contiguous: rows of 64 channels per key with the 128-byte swizzle, groups of 8 keys 1,024
+// bytes apart, the next 64 channels one panel on.
+__device__ __forceinline__ uint64_t desc_values(uint32_t addr) {
+  return (uint64_t)((addr & 0x3FFFFu) >> 4) | (uint64_t)(kPanel >> 4) << 16 | (uint64_t)(1024u >> 4) << 32 | (uint64_t)1 << 46 |
+         (uint64_t)2 << 61;
+}
+__host__ __device__ constexpr uint32_t idesc_f16(int n, bool b_n_contiguous) {
+  return (1u << 4) | (b_n_contiguous ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+}
+
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+// Four codes times r (a power of two up to 1) as fp16, exactly: (1024 + 128 + x) r - 1152 r for int8.
+template <bool E4M3>
+__device__ __forceinline__ void expand_scaled(uint32_t w, __half2 r, __half2 minus, uint32_t& lo, uint32_t& hi) {
+  if (E4M3) {
+    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}"
+        : "=r"(lo), "=r"(hi) : "r"(w));
+    const __half2 x = __hmul2(*reinterpret_cast<const __half2*>(&lo), r), y = __hmul2(*reinterpret_cast<const __half2*>(&hi), r);
+    lo = *reinterpret_cast<const uint32_t*>(&x);
+    hi = *reinterpret_cast<const uint32_t*>(&y);
+  } else {
+    w ^= 0x80808080u;
+    const uint32_t a = __byte_perm(w, 0x64646464u, 0x4140), b = __byte_perm(w, 0x64646464u, 0x4342);
+    const __half2 x = __hfma2(*reinterpret_cast<const __half2*>(&a), r, minus), y = __hfma2(*reinterpret_cast<const __half2*>(&b), r, minus);
+    lo = *reinterpret_cast<const uint32_t*>(&x);
+    hi = *reinterpret_cast<const uint32_t*>(&y);
+  }
+}
+
+// Chunk i of lane l: row and 16-byte chunk of 16 rows of codes.  The eight lanes of a phase of the 16-byte stores then write to eight
+// different bank groups of the swizzled operand, and a warp reads whole sectors.
+template <int D>
+__device__ __forceinline__ void place(int i, int l, int* row, int* chunk) {
+  if (D == 128) {
+    *row = (l & 1) | ((l & 2) << 1) | ((i & 1) << 1) | ((i >> 1) << 3);
+    *chunk = l >> 2;
+  } else if (D == 64) {
+    *row = (l & 1) | ((l & 2) << 1) | ((l >> 4) << 1) | (i << 3);
+    *chunk = (l >> 2) & 3;
+  } else if (D == 32) {
+    *row = (l & 1) | ((l & 2) << 1) | (((l >> 3) & 1) << 1) | ((l >> 4) << 3);
+    *chunk = (l >> 2) & 1;
+  } else {
+    const int x = 32 * i + l;
+    *row = x / (D / 16);
+    *chunk = x % (D / 16);
+  }
+}
+
+template <typename T, int D, bool E4M3>
+__global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_constant__ AttendArgs a, int* status) {
+  using S = Shape<T, D>;
+  constexpr int TILES = S::kTiles, LIMBS = S::kLimbs, ROWS = S::kRows;
+  constexpr uint32_t OP = S::kOperand;
+  extern __shared__ uint8_t raw_smem[];
+  uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw_smem) + 1023) & ~(uintptr_t)1023);
+  uint8_t* q_sm = base;                     // two operands
+  uint8_t* k_sm = base + 2 * OP;            // two stages
+  uint8_t* v_sm = base + 4 * OP;
+  Shared& sh = *reinterpret_cast<Shared*>(base + 6 * OP);
+  const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
+  volatile int* abort_flag = &sh.abort_flag;
+
+  if (t == 0) {
+    sh.abort_flag = 0;
+    tc::mbar_init(&sh.bar.q_ready, 128 * TILES);
+    tc::mbar_init(&sh.bar.o_done, 1);
+    tc::mbar_init(&sh.bar.drain, 1);
+    for (int i = 0; i < 2; ++i) {
+      tc::mbar_init(&sh.bar.k_full[i], 32 * kExpandWarps);
+      tc::mbar_init(&sh.bar.k_empty[i], 1);
+      tc::mbar_init(&sh.bar.v_full[i], 32 * kExpandWarps);
+      tc::mbar_init(&sh.bar.v_empty[i], 1);
+      tc::mbar_init(&sh.bar.s_ready[i], 1);
+      tc::mbar_init(&sh.bar.p_ready[i], 128);
+    }
+    tc::fence_barrier_init();
+  }
+  if (warp == kMmaWarp) tc::tmem_alloc(&sh.tmem, 512);
+  allow_successor();
+  wait_for_predecessor();
+  tc::tc_fence_before();
+  __syncthreads();
+  tc::tc_fence_after();
+  const uint32_t tmem = sh.tmem;
+  constexpr uint32_t O_COL = 256;           // S of the tiles at 0 and 128 (fp32: S, and P's low limb), O at 256 and 384
+
+  // ---- this CTA's run of units
+  int total = 0, before = 0, own = 0, upto = 0;
+  auto block_sum = [&](int v) -> int {      // by all threads: the total, and `upto`, the inclusive sum in order
+    int x = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, x, o);
+      if (lane >= o) x += y;
+    }
+    __syncthreads();
+    if (lane == 31) sh.sums[warp] = x;
+    __syncthreads();
+    int all = 0;
+    for (int w = 0; w < kThreads / 32; ++w) {
+      if (w < warp) x += sh.sums[w];
+      all += sh.sums[w];
+    }
+    upto = x;
+    return all;
+  };
+  auto units_of = [&](int b) -> int {
+    if (b >= a.b.nseq) return 0;
+    const Seq s = seq_of(a, b, ROWS);
+    return tiles_before(a, s, ROWS, s.blocks) * a.c.heads;
+  };
+#pragma unroll 1
+  for (int b0 = 0; b0 < a.b.nseq; b0 += kThreads) {
+    own = units_of(b0 + t);
+    total += block_sum(own);
+  }
+  const int per = max((total + (int)gridDim.x - 1) / (int)gridDim.x, 1);
+  const int u0 = (int)min((int64_t)blockIdx.x * per, (int64_t)total), u_end = min(total, u0 + per);
+  Meta* meta = a.meta + blockIdx.x;
+  if (t == 0) meta->last_cta = -1;
+  int item_at = 0;
+  Item it;
+  if (u0 < u_end) {
+#pragma unroll 1
+    for (int b0 = 0;; b0 += kThreads) {
+      int all = total;
+      if (a.b.nseq > kThreads) {
+        own = units_of(b0 + t);
+        all = block_sum(own);
+      }
+      if (before + all > u0) {
+        const int from = before + upto - own;
+        if (from <= u0 && u0 < from + own) {
+          sh.found[0] = b0 + t;
+          sh.found[1] = from;
+        }
+        __syncthreads();
+        break;
+      }
+      before += all;
+    }
+    it.b = sh.found[0];
+    it.s = seq_of(a, it.b, ROWS);
+    {
+      const int of_head = tiles_before(a, it.s, ROWS, it.s.blocks), rest = u0 - sh.found[1];
+      it.head = rest / of_head;
+      const int at = rest - it.head * of_head;
+      int lo = 0, hi = it.s.blocks - 1;     // the last block whose first unit is not behind u0
+#pragma unroll 1
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (tiles_before(a, it.s, ROWS, mid) <= at) lo = mid; else hi = mid - 1;
+      }
+      it.block = lo;
+      item_at = u0 - at + tiles_before(a, it.s, ROWS, lo);
+    }
+    describe(a, ROWS, &it);
+
+    int u = u0;
+    int n_item = 0, n_tile = 0;             // of this CTA, for phases and slots
+    bool ok = true;
+    auto wait_all = [&](uint64_t* bar, uint32_t parity) -> bool {   // one answer for the whole warp, which goes on together
+      const bool mine = tc::mbar_wait(bar, parity, abort_flag, status);
+      return __all_sync(0xffffffffu, mine);
+    };
+    if (warp < 4 * TILES) {
+      // ================================================================ softmax: thread r of group `tile` has row tile * 128 + r
+      const int tile = warp >> 2, r = t & 127;
+      const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+      const uint32_t s_col = lanes + 128 * tile, p_lo = lanes + 128, o_col = lanes + O_COL + 128 * tile;
+      while (u < u_end && ok) {
+        const int n = min(u_end, item_at + it.tiles) - u, first = u - item_at;
+        const int row = tile * 128 + r;
+        const bool mine = row < it.cols;
+        const int c = mine ? it.col0 + row : 0, q_head = it.head * a.g + c % a.g;
+        const int64_t q_row = it.row0 + c / a.g;
+        const int vis = mine ? seen_by(a, it.s, c) : it.vis_max;
+        float f;
+        {
+          const T* q = static_cast<const T*>(a.q) + q_row * a.ldq + (int64_t)q_head * a.hq;
+          uint32_t most = 0u;
+          if (mine)
+#pragma unroll 8
+            for (int i = 0; i < D; ++i) most = max(most, __float_as_uint((float)q[i]) & 0x7FFFFFFFu);
+          float inv;
+          const float s = query_scale(most, &inv);
+          f = most >= 0x7F800000u ? __uint_as_float(0x7FC00000u) : s * (a.scale * kLog2e);
+#pragma unroll 1
+          for (int i = 0; i < D / 8; ++i) {
+            uint32_t hi[4], lo_[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const float x = mine ? (float)q[8 * i + 2 * j] * inv : 0.f, y = mine ? (float)q[8 * i + 2 * j + 1] * inv : 0.f;
+              hi[j] = pack2(x, y);
+              const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&hi[j]));
+              lo_[j] = pack2(x - back.x, y - back.y);
+            }
+            const uint32_t at = (uint32_t)(i >> 3) * kPanel + (uint32_t)r * 128 + (uint32_t)(((i & 7) ^ (r & 7)) << 4);
+            *reinterpret_cast<uint4*>(q_sm + tile * OP + at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+            if (LIMBS == 2) *reinterpret_cast<uint4*>(q_sm + OP + at) = make_uint4(lo_[0], lo_[1], lo_[2], lo_[3]);
+          }
+        }
+        tc::fence_proxy_async();
+        tc::mbar_arrive(&sh.bar.q_ready);
+        float m = -TQ_INF, l = 0.f, uv = 0.f;
+        for (int i = 0; i < n && ok; ++i) {
+          const int nt = n_tile + i;
+          ok = wait_all(&sh.bar.s_ready[tile], nt & 1);
+          if (!ok) break;
+          tc::tc_fence_after();
+          if (i == 0) {                     // written before the item's first keys, which these scores have read
+            f *= sh.uk[n_item & 3];
+            uv = sh.uv[n_item & 3];
+          }
+          const int t0 = (first + i) * kKeys, flags = sh.flags[nt & 3];
+          const bool edge = t0 + kKeys > it.vis_min || flags != 0;
+          // keys of this tile that the row sees, 32 at a time
+          auto masked = [&](float x, int key) -> float {
+            return t0 + key >= vis || ((flags >> (8 + (key >> 4))) & 1) ? -TQ_INF : x;
+          };
+          float top = -TQ_INF;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            uint32_t v[32];
+            tc::tmem_ld32(s_col + 32 * j, v);
+            tc::tmem_ld_wait();
+            if (edge) {
+#pragma unroll
+              for (int e = 0; e < 32; ++e) top = fmaxf(top, masked(__uint_as_float(v[e]) * f, 32 * j + e));
+            } else {
+              float x0 = __uint_as_float(v[0]), x1 = x0;   // of the raw sums: f may have either sign
+#pragma unroll
+              for (int e = 1; e < 32; ++e) {
+                x0 = fmaxf(x0, __uint_as_float(v[e]));
+                x1 = fminf(x1, __uint_as_float(v[e]));
+              }
+              top = fmaxf(top, fmaxf(x0 * f, x1 * f));
+            }
+          }
+          const bool higher = top > m + kSlack;
+          if (__any_sync(0xffffffffu, higher)) {
+            float alpha = 1.f;
+            if (higher) {
+              alpha = ex2(m - top);         // 0 for the first
+              m = top;
+              l *= alpha;
+            }
+            if (i > 0) {                    // O holds nothing before the first tile
+#pragma unroll 1
+              for (int j = 0; j < D / 32; ++j) {
+                uint32_t v[32];
+                tc::tmem_ld32(o_col + 32 * j, v);
+                tc::tmem_ld_wait();
+#pragma unroll
+                for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * alpha);
+                tc::tmem_st32(o_col + 32 * j, v);
+              }
+            }
+          }
+          const float shift = m == -TQ_INF ? 0.f : kLift - m;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            uint32_t v[32], p[16], pl[16];
+            tc::tmem_ld32(s_col + 32 * j, v);
+            tc::tmem_ld_wait();
+            if (edge) {
+#pragma unroll
+              for (int e = 0; e < 32; ++e) {
+                float x = masked(__uint_as_float(v[e]) * f, 32 * j + e);
+                x = ex2(x + shift);
+                // values of a NaN block are zeros in the operand: the weight carries the NaN to the rows that see the block
+                if (((flags >> ((32 * j + e) >> 4)) & 1) && t0 + 32 * j + e < vis) x = __uint_as_float(0x7FC00000u);
+                v[e] = __float_as_uint(x);
+              }
+            } else {
+#pragma unroll
+              for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(ex2(fmaf(__uint_as_float(v[e]), f, shift)));
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const float x = __uint_as_float(v[2 * e]), y = __uint_as_float(v[2 * e + 1]);
+              l += x + y;
+              p[e] = pack2(x, y);
+              if (LIMBS == 2) {
+                const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&p[e]));
+                pl[e] = pack2(x - back.x, y - back.y);
+              }
+            }
+            tmem_st16(s_col + 16 * j, p);   // over columns of S that have been read
+            if (LIMBS == 2) tmem_st16(p_lo + 16 * j, pl);
+          }
+          tc::tmem_st_wait();
+          tc::tc_fence_before();
+          tc::mbar_arrive(&sh.bar.p_ready[tile]);
+        }
+        if (ok) ok = wait_all(&sh.bar.o_done, n_item & 1);
+        const bool good = ok;
+        tc::tc_fence_after();
+        const bool whole = u == item_at && u + n == item_at + it.tiles;
+        const int slot = 2 * (int)blockIdx.x + (u == item_at ? 1 : 0);
+        const float by = !good ? __uint_as_float(0x7FC00000u) : (whole ? (l == 0.f ? 0.f : uv / l) : uv);
+        T* out = static_cast<T*>(a.out) + q_row * a.ldo + (int64_t)q_head * a.ho;
+        float* part = a.part_o + ((int64_t)slot * a.pitch + row) * D;
+#pragma unroll 1
+        for (int j = 0; j < D / 32; ++j) {
+          uint32_t v[32];
+          tc::tmem_ld32(o_col + 32 * j, v);
+          tc::tmem_ld_wait();
+          if (mine) {
+            if (whole) {
+#pragma unroll
+              for (int e = 0; e < 32; ++e) store_out<T>(out + 32 * j + e, l == 0.f && good ? 0.f : __uint_as_float(v[e]) * by);
+            } else {
+#pragma unroll
+              for (int e = 0; e < 32; ++e) part[32 * j + e] = __uint_as_float(v[e]) * by;
+            }
+          }
+        }
+        if (mine) {
+          if (!whole) {
+            a.part_ml[(int64_t)slot * 2 * a.pitch + row] = m;
+            a.part_ml[(int64_t)slot * 2 * a.pitch + a.pitch + row] = good ? l : by;
+          } else if (a.lse) {
+            a.lse[q_row * ((int64_t)a.c.heads * a.g) + q_head] =
+                !good ? by : (l == 0.f ? -TQ_INF : (m == -TQ_INF ? 0.f : (m - kLift) * kLn2) + logf(l));
+          }
+        }
+        if (!whole && u == item_at && t == 0) {
+          meta->row0 = it.row0;
+          meta->col0 = it.col0;
+          meta->cols = it.cols;
+          meta->head = it.head;
+          meta->last_cta = (item_at + it.tiles - 1) / per;
+        }
+        tc::tc_fence_before();
+        n_tile += n;
+        ++n_item;
+        u += n;
+        item_at += it.tiles;
+        if (u < u_end) next_item(a, ROWS, &it);
+      }
+    } else if (warp >= kExpandWarp0 && warp < kMmaWarp) {
+      // ================================================================ codes -> fp16 operands
+      const int we = warp - kExpandWarp0;   // takes keys 16 g .. 16 g + 15 of a tile for g = we, we + 3, we + 6
+      constexpr int G = (8 + kExpandWarps - 1) / kExpandWarps, N = D / 32;   // 16-byte chunks per lane of 16 keys
+      while (u < u_end && ok) {
+        const int n = min(u_end, item_at + it.tiles) - u, first = u - item_at;
+        const int32_t* row_pages = a.b.table + (int64_t)it.b * a.b.ldt;
+        // largest scales of the pages in hand
+        float top_k = 0.f, top_v = 0.f;
+        {
+          const int64_t t_first = (int64_t)first * kKeys, t_last = min((int64_t)(first + n) * kKeys, (int64_t)it.vis_max);
+          if (t_last > t_first)
+#pragma unroll 4
+            for (int64_t j = (t_first >> a.c.page_shift) + lane; j <= (t_last - 1) >> a.c.page_shift; j += 32) {
+              const int id = row_pages[j];
+              const bool is = id >= 0 && id < a.c.pages;
+              const int64_t at = (int64_t)(is ? id : 0) * a.c.heads + it.head;
+              const float x = a.c.k_scale[at], y = a.c.v_scale[at];
+              top_k = is ? fmaxf(top_k, x) : top_k;   // NaN is passed over
+              top_v = is ? fmaxf(top_v, y) : top_v;
+            }
+#pragma unroll
+          for (int o = 16; o > 0; o >>= 1) {
+            top_k = fmaxf(top_k, __shfl_xor_sync(0xffffffffu, top_k, o));
+            top_v = fmaxf(top_v, __shfl_xor_sync(0xffffffffu, top_v, o));
+          }
+        }
+        if (we == 0 && lane == 0) {
+          sh.uk[n_item & 3] = top_k;
+          sh.uv[n_item & 3] = top_v;
+        }
+        const float inv_k = block_inverse(top_k), inv_v = block_inverse(top_v);
+        uint4 kr[G][N], vr[G][N];
+        // what lane l < 8 knows of keys 16 l .. 16 l + 15 of a tile: page, ratios of the scales
+        int pid = -1;
+        float rk = 0.f, rv = 0.f;
+        auto look_up = [&](int tile_no) {
+          pid = -1;
+          const int64_t t0 = (int64_t)tile_no * kKeys + 16 * (lane & 7);
+          if (tile_no < first + n && t0 < it.vis_max) {
+            const int id = row_pages[t0 >> a.c.page_shift];
+            if (id >= 0 && id < a.c.pages) pid = id;
+          }
+          rk = pid >= 0 ? a.c.k_scale[(int64_t)pid * a.c.heads + it.head] * inv_k : 0.f;
+          rv = pid >= 0 ? a.c.v_scale[(int64_t)pid * a.c.heads + it.head] * inv_v : 0.f;
+        };
+        auto read = [&](const uint8_t* codes, int tile_no, uint4 (&x)[G][N]) {
+#pragma unroll
+          for (int g = 0; g < G; ++g) {
+            const int grp = we + kExpandWarps * g, id = __shfl_sync(0xffffffffu, pid, grp & 7);
+            const int t0 = tile_no * kKeys + 16 * grp;
+            const uint8_t* from = codes + (((int64_t)id * a.c.heads + it.head) << a.c.page_shift) * D + (t0 & ((1 << a.c.page_shift) - 1)) * D;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+              int row, chunk;
+              place<D>(i, lane, &row, &chunk);
+              x[g][i] = make_uint4(0u, 0u, 0u, 0u);
+              if (grp < 8 && id >= 0 && t0 + row < it.vis_max) x[g][i] = __ldg(reinterpret_cast<const uint4*>(from + row * D + 16 * chunk));
+            }
+          }
+        };
+        auto write = [&](uint8_t* operand, const uint4 (&x)[G][N], float ratio, bool zero_nan) {
+#pragma unroll
+          for (int g = 0; g < G; ++g) {
+            const int grp = we + kExpandWarps * g;
+            float r = __shfl_sync(0xffffffffu, ratio, grp & 7);
+            if (grp >= 8) continue;
+            if (zero_nan && !(r == r)) r = 0.f;
+            const __half2 r2 = __float2half2_rn(r), minus = __float2half2_rn(-1152.f * r);
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+              int row, chunk;
+              place<D>(i, lane, &row, &chunk);
+              const uint32_t w[4] = {x[g][i].x, x[g][i].y, x[g][i].z, x[g][i].w};
+              uint32_t y[8];
+#pragma unroll
+              for (int j = 0; j < 4; ++j) expand_scaled<E4M3>(w[j], r2, minus, y[2 * j], y[2 * j + 1]);
+              uint8_t* to = operand + (uint32_t)(chunk >> 2) * kPanel + (uint32_t)(16 * grp + row) * 128;
+              const int piece = (chunk & 3) * 2;
+              *reinterpret_cast<uint4*>(to + ((piece ^ (row & 7)) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
+              *reinterpret_cast<uint4*>(to + (((piece + 1) ^ (row & 7)) << 4)) = make_uint4(y[4], y[5], y[6], y[7]);
+            }
+          }
+        };
+        look_up(first);
+        read(a.c.k, first, kr);
+        read(a.c.v, first, vr);
+        for (int i = 0; i < n && ok; ++i) {
+          const int nt = n_tile + i, st = nt & 1;
+          const uint32_t phase = ((nt >> 1) & 1) ^ 1;
+          const float rk_now = rk, rv_now = rv;
+          // slots of no page (those behind the last token are masked anyway), and NaN values
+          const uint32_t absent = __ballot_sync(0xffffffffu, lane < 8 && pid < 0), nan = __ballot_sync(0xffffffffu, lane < 8 && !(rv == rv));
+          look_up(first + i + 1);
+          ok = wait_all(&sh.bar.k_empty[st], phase);
+          if (!ok) break;
+          if (we == 0 && lane == 0) sh.flags[nt & 3] = (int)(((absent & 0xFFu) << 8) | (nan & 0xFFu));
+          write(k_sm + st * OP, kr, rk_now, false);
+          tc::fence_proxy_async();
+          tc::mbar_arrive(&sh.bar.k_full[st]);
+          read(a.c.k, first + i + 1, kr);
+          ok = wait_all(&sh.bar.v_empty[st], phase);
+          if (!ok) break;
+          write(v_sm + st * OP, vr, rv_now, true);
+          tc::fence_proxy_async();
+          tc::mbar_arrive(&sh.bar.v_full[st]);
+          read(a.c.v, first + i + 1, vr);
+        }
+        n_tile += n;
+        ++n_item;
+        u += n;
+        item_at += it.tiles;
+        if (u < u_end) next_item(a, ROWS, &it);
+      }
+    } else if (warp == kMmaWarp && lane == 0) {
+      // ================================================================ MMAs
+      constexpr uint32_t id_s = idesc_f16(kKeys, false), id_o = idesc_f16(D, true);
+      const uint32_t q_at = tc::smem_u32(q_sm), k_at = tc::smem_u32(k_sm), v_at = tc::smem_u32(v_sm);
+      auto scores = [&](int tile, int st) {
+#pragma unroll
+        for (int x = 0; x < LIMBS; ++x)
+#pragma unroll
+          for (int k = 0; k < D / 16; ++k) {
+            const uint32_t off = (uint32_t)(k >> 2) * kPanel + (uint32_t)(k & 3) * 32;
+            tc::umma_bf16(tmem + 128 * tile, tc::smem_desc_sw128(q_at + (tile + x) * OP + off), tc::smem_desc_sw128(k_at + st * OP + off), id_s,
+                          (x | k) != 0 ? 1u : 0u);
+          }
+      };
+      auto sums = [&](int tile, int st, bool fresh) {
+#pragma unroll
+        for (int x = 0; x < LIMBS; ++x)
+#pragma unroll
+          for (int k = 0; k < kKeys / 16; ++k)
+            umma_f16_ts(tmem + O_COL + 128 * tile, tmem + 128 * (tile + x) + 8 * k, desc_values(v_at + st * OP + 2048 * k), id_o,
+                        !fresh || (x | k) != 0 ? 1u : 0u);
+      };
+      while (u < u_end && ok) {
+        const int n = min(u_end, item_at + it.tiles) - u;
+        ok = tc::mbar_wait(&sh.bar.q_ready, n_item & 1, abort_flag, status) &&
+             tc::mbar_wait(&sh.bar.k_full[n_tile & 1], (n_tile >> 1) & 1, abort_flag, status);
+        if (!ok) break;
+        tc::tc_fence_after();
+#pragma unroll
+        for (int tile = 0; tile < TILES; ++tile) {
+          scores(tile, n_tile & 1);
+          tc::umma_commit(&sh.bar.s_ready[tile]);
+        }
+        tc::umma_commit(&sh.bar.k_empty[n_tile & 1]);
+        for (int i = 0; i < n && ok; ++i) {
+          const int nt = n_tile + i, st = nt & 1;
+#pragma unroll
+          for (int tile = 0; tile < TILES; ++tile) {
+            ok = ok && tc::mbar_wait(&sh.bar.p_ready[tile], nt & 1, abort_flag, status);
+            if (tile == 0) ok = ok && tc::mbar_wait(&sh.bar.v_full[st], (nt >> 1) & 1, abort_flag, status);
+            if (!ok) break;
+            tc::tc_fence_after();
+            sums(tile, st, i == 0);
+            if (i + 1 < n) {
+              if (tile == 0) ok = tc::mbar_wait(&sh.bar.k_full[(nt + 1) & 1], ((nt + 1) >> 1) & 1, abort_flag, status);
+              if (!ok) break;
+              tc::tc_fence_after();
+              scores(tile, (nt + 1) & 1);
+              tc::umma_commit(&sh.bar.s_ready[tile]);
+            }
+          }
+          if (!ok) break;
+          tc::umma_commit(&sh.bar.v_empty[st]);
+          if (i + 1 < n) tc::umma_commit(&sh.bar.k_empty[(nt + 1) & 1]);
+        }
+        if (ok) tc::umma_commit(&sh.bar.o_done);
+        n_tile += n;
+        ++n_item;
+        u += n;
+        item_at += it.tiles;
+        if (u < u_end) next_item(a, ROWS, &it);
+      }
+      if (!ok) {   // what was issued still reads shared memory and writes TMEM (else the softmax groups have waited for the last commit)
+        volatile int never = 0;
+        tc::umma_commit(&sh.bar.drain);
+        tc::mbar_wait_slow(&sh.bar.drain, 0, &never, status);
+      }
+    }
+  }
+  __syncwarp();
+  tc::tc_fence_before();
+  __syncthreads();
+  tc::tc_fence_after();
+  if (warp == kMmaWarp) tc::tmem_dealloc(tmem, 512);
+}
+
+template <typename T, int D, bool E4M3>
+cudaError_t launch(const AttendArgs& a, int* status, int sms, cudaStream_t st) {
+  static std::atomic<unsigned long long> devices{0};
+  const cudaError_t e = allow_largest_smem(reinterpret_cast<const void*>(prompt_kernel<T, D, E4M3>), devices);
+  if (e != cudaSuccess) return e;
+  return launch_dependent(prompt_kernel<T, D, E4M3>, dim3((unsigned)sms), dim3(kThreads), Shape<T, D>::smem, st, a, status);
+}
+template <typename T>
+cudaError_t launch_t(const AttendArgs& a, bool e4m3, int* status, int sms, cudaStream_t st) {
+  switch (a.c.d) {
+    case 32: return e4m3 ? launch<T, 32, true>(a, status, sms, st) : launch<T, 32, false>(a, status, sms, st);
+    case 64: return e4m3 ? launch<T, 64, true>(a, status, sms, st) : launch<T, 64, false>(a, status, sms, st);
+    case 96: return e4m3 ? launch<T, 96, true>(a, status, sms, st) : launch<T, 96, false>(a, status, sms, st);
+    default: return e4m3 ? launch<T, 128, true>(a, status, sms, st) : launch<T, 128, false>(a, status, sms, st);
+  }
+}
+
+struct Space {
+  size_t ml, o, status, bytes;
+};
+Space lay_out(int sms, int d) {
+  Space s;
+  s.ml = (size_t)round_up64((int64_t)sms * sizeof(Meta), 256);
+  s.o = s.ml + (size_t)round_up64((int64_t)sms * 2 * 2 * kPromptRows * sizeof(float), 256);
+  s.status = s.o + (size_t)sms * 2 * kPromptRows * d * sizeof(float);
+  s.bytes = s.status + 256;
+  return s;
+}
+
+}  // namespace
+
+size_t prompt_space(int sms, int d) { return lay_out(sms, d).bytes; }
+
+cudaError_t launch_prompt(AttendArgs& a, int dtype, bool e4m3, int sms, void* workspace, cudaStream_t st) {
+  const Space s = lay_out(sms, a.c.d);
+  char* w = static_cast<char*>(workspace);
+  a.meta = reinterpret_cast<Meta*>(w);
+  a.part_ml = reinterpret_cast<float*>(w + s.ml);
+  a.part_o = reinterpret_cast<float*>(w + s.o);
+  a.pitch = kPromptRows;
+  int* status = reinterpret_cast<int*>(w + s.status);   // only written: a CTA whose wait ran out says so with NaN
+  const cudaError_t e = dtype == TQ_F32 ? launch_t<float>(a, e4m3, status, sms, st) : launch_t<__nv_bfloat16>(a, e4m3, status, sms, st);
+  if (e != cudaSuccess) return e;
+  return launch_join(a, dtype, sms, (dtype == TQ_F32 ? 128 : 256) / 8, st);
+}
+
+}  // namespace kv8
+}  // namespace tq

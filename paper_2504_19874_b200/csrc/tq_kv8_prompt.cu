@@ -173,6 +173,72 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   const __half2 h = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&h);
 }
+// Two fp32 operations at a time.
+__device__ __forceinline__ uint64_t both(float x) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %1};" : "=l"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ void fma2(uint32_t& x, uint32_t& y, uint64_t f, uint64_t c) {
+  uint64_t v;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "r"(x), "r"(y));
+  asm("fma.rn.f32x2 %0, %0, %1, %2;" : "+l"(v) : "l"(f), "l"(c));
+  asm("mov.b64 {%0, %1}, %2;" : "=r"(x), "=r"(y) : "l"(v));
+}
+__device__ __forceinline__ void add2(uint64_t& s, float x, float y) {
+  uint64_t v;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(x), "f"(y));
+  asm("add.rn.f32x2 %0, %0, %1;" : "+l"(s) : "l"(v));
+}
+__device__ __forceinline__ float sum_of(uint64_t s) {
+  float x, y;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(s));
+  return x + y;
+}
+// Eight consecutive elements of a row of queries; `vec`: the row is 16-byte aligned.
+template <typename T>
+__device__ __forceinline__ void row8(const T* p, bool vec, float (&x)[8]) {
+  if (!vec) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = (float)p[i];
+  } else if (sizeof(T) == 4) {
+    const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
+    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+  } else {
+    const uint4 a = __ldg(reinterpret_cast<const uint4*>(p));
+    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = __uint_as_float(w[i] << 16);
+      x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+  }
+}
+// 32 consecutive results of a row.
+template <typename T>
+__device__ __forceinline__ void store32(T* p, bool vec, const uint32_t (&v)[32], float by) {
+  if (!vec) {
+#pragma unroll
+    for (int e = 0; e < 32; ++e) store_out<T>(p + e, __uint_as_float(v[e]) * by);
+  } else if (sizeof(T) == 4) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      reinterpret_cast<float4*>(p)[e] = make_float4(__uint_as_float(v[4 * e]) * by, __uint_as_float(v[4 * e + 1]) * by,
+                                                    __uint_as_float(v[4 * e + 2]) * by, __uint_as_float(v[4 * e + 3]) * by);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      uint32_t w[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float(v[8 * e + 2 * j]) * by, __uint_as_float(v[8 * e + 2 * j + 1]) * by);
+        w[j] = *reinterpret_cast<const uint32_t*>(&h);
+      }
+      reinterpret_cast<uint4*>(p)[e] = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  }
+}
+
 // Four codes times r (a power of two up to 1) as fp16, exactly: (1024 + 128 + x) r - 1152 r for int8.
 template <bool E4M3>
 __device__ __forceinline__ void expand_scaled(uint32_t w, __half2 r, __half2 minus, uint32_t& lo, uint32_t& hi) {
@@ -343,22 +409,34 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
         float f;
         {
           const T* q = static_cast<const T*>(a.q) + q_row * a.ldq + (int64_t)q_head * a.hq;
+          const bool vec = (reinterpret_cast<uintptr_t>(q) & 15) == 0;
           uint32_t most = 0u;
           if (mine)
-#pragma unroll 8
-            for (int i = 0; i < D; ++i) most = max(most, __float_as_uint((float)q[i]) & 0x7FFFFFFFu);
+#pragma unroll 4
+            for (int i = 0; i < D / 8; ++i) {
+              float x[8];
+              row8(q + 8 * i, vec, x);
+#pragma unroll
+              for (int j = 0; j < 8; ++j) most = max(most, __float_as_uint(x[j]) & 0x7FFFFFFFu);
+            }
           float inv;
           const float s = query_scale(most, &inv);
-          f = most >= 0x7F800000u ? __uint_as_float(0x7FC00000u) : s * (a.scale * kLog2e);
-#pragma unroll 1
+          // a negative scale goes into the queries: the largest sum is then the largest score
+          f = most >= 0x7F800000u ? __uint_as_float(0x7FC00000u) : s * fabsf(a.scale * kLog2e);
+          inv = a.scale < 0.f ? -inv : inv;
+#pragma unroll 4
           for (int i = 0; i < D / 8; ++i) {
+            float x[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = 0.f;
+            if (mine) row8(q + 8 * i, vec, x);
             uint32_t hi[4], lo_[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-              const float x = mine ? (float)q[8 * i + 2 * j] * inv : 0.f, y = mine ? (float)q[8 * i + 2 * j + 1] * inv : 0.f;
-              hi[j] = pack2(x, y);
+              const float y = x[2 * j] * inv, z = x[2 * j + 1] * inv;
+              hi[j] = pack2(y, z);
               const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&hi[j]));
-              lo_[j] = pack2(x - back.x, y - back.y);
+              lo_[j] = pack2(y - back.x, z - back.y);
             }
             const uint32_t at = (uint32_t)(i >> 3) * kPanel + (uint32_t)r * 128 + (uint32_t)(((i & 7) ^ (r & 7)) << 4);
             *reinterpret_cast<uint4*>(q_sm + tile * OP + at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
@@ -379,28 +457,34 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
           }
           const int t0 = (first + i) * kKeys, flags = sh.flags[nt & 3];
           const bool edge = t0 + kKeys > it.vis_min || flags != 0;
-          // keys of this tile that the row sees, 32 at a time
-          auto masked = [&](float x, int key) -> float {
-            return t0 + key >= vis || ((flags >> (8 + (key >> 4))) & 1) ? -TQ_INF : x;
-          };
-          float top = -TQ_INF;
+          uint32_t v[4][32];
+          auto load_scores = [&] {
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            uint32_t v[32];
-            tc::tmem_ld32(s_col + 32 * j, v);
+            for (int j = 0; j < 4; ++j) tc::tmem_ld32(s_col + 32 * j, v[j]);
             tc::tmem_ld_wait();
-            if (edge) {
+          };
+          load_scores();
+          // keys that the row does not see: -inf
+          auto mask = [&] {
 #pragma unroll
-              for (int e = 0; e < 32; ++e) top = fmaxf(top, masked(__uint_as_float(v[e]) * f, 32 * j + e));
-            } else {
-              float x0 = __uint_as_float(v[0]), x1 = x0;   // of the raw sums: f may have either sign
+            for (int j = 0; j < 4; ++j)
 #pragma unroll
-              for (int e = 1; e < 32; ++e) {
-                x0 = fmaxf(x0, __uint_as_float(v[e]));
-                x1 = fminf(x1, __uint_as_float(v[e]));
-              }
-              top = fmaxf(top, fmaxf(x0 * f, x1 * f));
-            }
+              for (int e = 0; e < 32; ++e)
+                if (t0 + 32 * j + e >= vis || ((flags >> (8 + ((32 * j + e) >> 4))) & 1)) v[j][e] = 0xFF800000u;
+          };
+          if (edge) mask();
+          float top = -TQ_INF;
+          {
+            float x[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] = __uint_as_float(v[j][0]);
+#pragma unroll
+            for (int e = 1; e < 31; e += 2)
+#pragma unroll
+              for (int j = 0; j < 4; ++j) x[j] = fmaxf(fmaxf(x[j], __uint_as_float(v[j][e])), __uint_as_float(v[j][e + 1]));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) top = fmaxf(top, fmaxf(x[j], __uint_as_float(v[j][31])));
+            top = top == -TQ_INF ? top : top * f;
           }
           const bool higher = top > m + kSlack;
           if (__any_sync(0xffffffffu, higher)) {
@@ -413,47 +497,45 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
             if (i > 0) {                    // O holds nothing before the first tile
 #pragma unroll 1
               for (int j = 0; j < D / 32; ++j) {
-                uint32_t v[32];
-                tc::tmem_ld32(o_col + 32 * j, v);
+                tc::tmem_ld32(o_col + 32 * j, v[0]);
                 tc::tmem_ld_wait();
 #pragma unroll
-                for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * alpha);
-                tc::tmem_st32(o_col + 32 * j, v);
+                for (int e = 0; e < 32; ++e) v[0][e] = __float_as_uint(__uint_as_float(v[0][e]) * alpha);
+                tc::tmem_st32(o_col + 32 * j, v[0]);
               }
+              load_scores();                // S is still there, and registers are scarce
+              if (edge) mask();
             }
           }
           const float shift = m == -TQ_INF ? 0.f : kLift - m;
+          const uint64_t f2 = both(f), shift2 = both(shift);
+          uint64_t sum[2] = {0ull, 0ull};
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            uint32_t v[32], p[16], pl[16];
-            tc::tmem_ld32(s_col + 32 * j, v);
-            tc::tmem_ld_wait();
-            if (edge) {
+            uint32_t p[16], pl[16];
 #pragma unroll
-              for (int e = 0; e < 32; ++e) {
-                float x = masked(__uint_as_float(v[e]) * f, 32 * j + e);
-                x = ex2(x + shift);
+            for (int e = 0; e < 32; e += 2) {
+              // -inf times f may be NaN where f is 0: masked scores stay out of the product
+              const bool out0 = edge && v[j][e] == 0xFF800000u, out1 = edge && v[j][e + 1] == 0xFF800000u;
+              fma2(v[j][e], v[j][e + 1], f2, shift2);
+              float x = ex2(__uint_as_float(v[j][e])), y = ex2(__uint_as_float(v[j][e + 1]));
+              if (edge) {
+                x = out0 ? 0.f : x;
+                y = out1 ? 0.f : y;
                 // values of a NaN block are zeros in the operand: the weight carries the NaN to the rows that see the block
                 if (((flags >> ((32 * j + e) >> 4)) & 1) && t0 + 32 * j + e < vis) x = __uint_as_float(0x7FC00000u);
-                v[e] = __float_as_uint(x);
               }
-            } else {
-#pragma unroll
-              for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(ex2(fmaf(__uint_as_float(v[e]), f, shift)));
-            }
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const float x = __uint_as_float(v[2 * e]), y = __uint_as_float(v[2 * e + 1]);
-              l += x + y;
-              p[e] = pack2(x, y);
+              add2(sum[(e >> 1) & 1], x, y);
+              p[e >> 1] = pack2(x, y);
               if (LIMBS == 2) {
-                const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&p[e]));
-                pl[e] = pack2(x - back.x, y - back.y);
+                const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&p[e >> 1]));
+                pl[e >> 1] = pack2(x - back.x, y - back.y);
               }
             }
             tmem_st16(s_col + 16 * j, p);   // over columns of S that have been read
             if (LIMBS == 2) tmem_st16(p_lo + 16 * j, pl);
           }
+          l += sum_of(sum[0]) + sum_of(sum[1]);
           tc::tmem_st_wait();
           tc::tc_fence_before();
           tc::mbar_arrive(&sh.bar.p_ready[tile]);
@@ -465,6 +547,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
         const int slot = 2 * (int)blockIdx.x + (u == item_at ? 1 : 0);
         const float by = !good ? __uint_as_float(0x7FC00000u) : (whole ? (l == 0.f ? 0.f : uv / l) : uv);
         T* out = static_cast<T*>(a.out) + q_row * a.ldo + (int64_t)q_head * a.ho;
+        const bool vec_out = (reinterpret_cast<uintptr_t>(out) & 15) == 0;
         float* part = a.part_o + ((int64_t)slot * a.pitch + row) * D;
 #pragma unroll 1
         for (int j = 0; j < D / 32; ++j) {
@@ -473,11 +556,13 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
           tc::tmem_ld_wait();
           if (mine) {
             if (whole) {
+              if (l == 0.f && good) {
 #pragma unroll
-              for (int e = 0; e < 32; ++e) store_out<T>(out + 32 * j + e, l == 0.f && good ? 0.f : __uint_as_float(v[e]) * by);
+                for (int e = 0; e < 32; ++e) v[e] = 0u;
+              }
+              store32<T>(out + 32 * j, vec_out, v, by);
             } else {
-#pragma unroll
-              for (int e = 0; e < 32; ++e) part[32 * j + e] = __uint_as_float(v[e]) * by;
+              store32<float>(part + 32 * j, true, v, by);
             }
           }
         }
@@ -537,31 +622,44 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
         }
         const float inv_k = block_inverse(top_k), inv_v = block_inverse(top_v);
         uint4 kr[G][N], vr[G][N];
-        // what lane l < 8 knows of keys 16 l .. 16 l + 15 of a tile: page, ratios of the scales
-        int pid = -1;
-        float rk = 0.f, rv = 0.f;
-        auto look_up = [&](int tile_no) {
-          pid = -1;
+        // what lane l < 8 knows of keys 16 l .. 16 l + 15 of a tile: page and scales; looked up two tiles ahead
+        struct Known { int id; float ks, vs; };
+        auto look_up = [&](int tile_no) -> Known {
+          Known x{-1, 0.f, 0.f};
           const int64_t t0 = (int64_t)tile_no * kKeys + 16 * (lane & 7);
           if (tile_no < first + n && t0 < it.vis_max) {
             const int id = row_pages[t0 >> a.c.page_shift];
-            if (id >= 0 && id < a.c.pages) pid = id;
+            if (id >= 0 && id < a.c.pages) {
+              x.id = id;
+              x.ks = a.c.k_scale[(int64_t)id * a.c.heads + it.head];
+              x.vs = a.c.v_scale[(int64_t)id * a.c.heads + it.head];
+            }
           }
-          rk = pid >= 0 ? a.c.k_scale[(int64_t)pid * a.c.heads + it.head] * inv_k : 0.f;
-          rv = pid >= 0 ? a.c.v_scale[(int64_t)pid * a.c.heads + it.head] * inv_v : 0.f;
+          return x;
         };
-        auto read = [&](const uint8_t* codes, int tile_no, uint4 (&x)[G][N]) {
+        const int64_t head_bytes = (int64_t)D << a.c.page_shift, page_bytes = head_bytes * a.c.heads;
+        const uint8_t *k_head = a.c.k + it.head * head_bytes, *v_head = a.c.v + it.head * head_bytes;
+        auto read = [&](const uint8_t* codes, int id8, int tile_no, uint4 (&x)[G][N]) {
 #pragma unroll
           for (int g = 0; g < G; ++g) {
-            const int grp = we + kExpandWarps * g, id = __shfl_sync(0xffffffffu, pid, grp & 7);
+            const int grp = we + kExpandWarps * g, id = __shfl_sync(0xffffffffu, id8, grp & 7);
             const int t0 = tile_no * kKeys + 16 * grp;
-            const uint8_t* from = codes + (((int64_t)id * a.c.heads + it.head) << a.c.page_shift) * D + (t0 & ((1 << a.c.page_shift) - 1)) * D;
+            const uint8_t* from = codes + id * page_bytes + (t0 & ((1 << a.c.page_shift) - 1)) * D;
+            if (grp < 8 && id >= 0 && t0 + 16 <= it.vis_max) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-              int row, chunk;
-              place<D>(i, lane, &row, &chunk);
-              x[g][i] = make_uint4(0u, 0u, 0u, 0u);
-              if (grp < 8 && id >= 0 && t0 + row < it.vis_max) x[g][i] = __ldg(reinterpret_cast<const uint4*>(from + row * D + 16 * chunk));
+              for (int i = 0; i < N; ++i) {
+                int row, chunk;
+                place<D>(i, lane, &row, &chunk);
+                x[g][i] = __ldg(reinterpret_cast<const uint4*>(from + row * D + 16 * chunk));
+              }
+            } else {                        // no page, or keys behind the last one: zeros
+#pragma unroll
+              for (int i = 0; i < N; ++i) {
+                int row, chunk;
+                place<D>(i, lane, &row, &chunk);
+                x[g][i] = make_uint4(0u, 0u, 0u, 0u);
+                if (grp < 8 && id >= 0 && t0 + row < it.vis_max) x[g][i] = __ldg(reinterpret_cast<const uint4*>(from + row * D + 16 * chunk));
+              }
             }
           }
         };
@@ -588,29 +686,30 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
             }
           }
         };
-        look_up(first);
-        read(a.c.k, first, kr);
-        read(a.c.v, first, vr);
+        Known now = look_up(first), next = look_up(first + 1);
+        read(k_head, now.id, first, kr);
+        read(v_head, now.id, first, vr);
         for (int i = 0; i < n && ok; ++i) {
           const int nt = n_tile + i, st = nt & 1;
           const uint32_t phase = ((nt >> 1) & 1) ^ 1;
-          const float rk_now = rk, rv_now = rv;
+          const float rk = now.id >= 0 ? now.ks * inv_k : 0.f, rv = now.id >= 0 ? now.vs * inv_v : 0.f;
           // slots of no page (those behind the last token are masked anyway), and NaN values
-          const uint32_t absent = __ballot_sync(0xffffffffu, lane < 8 && pid < 0), nan = __ballot_sync(0xffffffffu, lane < 8 && !(rv == rv));
-          look_up(first + i + 1);
+          const uint32_t absent = __ballot_sync(0xffffffffu, lane < 8 && now.id < 0), nan = __ballot_sync(0xffffffffu, lane < 8 && !(rv == rv));
+          now = next;
+          next = look_up(first + i + 2);
           ok = wait_all(&sh.bar.k_empty[st], phase);
           if (!ok) break;
           if (we == 0 && lane == 0) sh.flags[nt & 3] = (int)(((absent & 0xFFu) << 8) | (nan & 0xFFu));
-          write(k_sm + st * OP, kr, rk_now, false);
+          write(k_sm + st * OP, kr, rk, false);
           tc::fence_proxy_async();
           tc::mbar_arrive(&sh.bar.k_full[st]);
-          read(a.c.k, first + i + 1, kr);
+          read(k_head, now.id, first + i + 1, kr);
           ok = wait_all(&sh.bar.v_empty[st], phase);
           if (!ok) break;
-          write(v_sm + st * OP, vr, rv_now, true);
+          write(v_sm + st * OP, vr, rv, true);
           tc::fence_proxy_async();
           tc::mbar_arrive(&sh.bar.v_full[st]);
-          read(a.c.v, first + i + 1, vr);
+          read(v_head, now.id, first + i + 1, vr);
         }
         n_tile += n;
         ++n_item;

@@ -16,6 +16,7 @@
 // other.  Waits are bounded; a CTA that gives up writes NaN.
 #include <algorithm>
 #include <cstring>
+#include <type_traits>
 
 #include "tq_kv8.h"
 #include "tq_kv8_attend.h"
@@ -453,6 +454,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
           tc::tc_fence_after();
           if (i == 0) {                     // written before the item's first keys, which these scores have read
             f *= sh.uk[n_item & 3];
+            if (f < 1e-30f) f = 1e-30f;     // keys of zeros, or no scale: all scores are (nearly) 0, and -inf stays what it is
             uv = sh.uv[n_item & 3];
           }
           const int t0 = (first + i) * kKeys, flags = sh.flags[nt & 3];
@@ -484,7 +486,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
               for (int j = 0; j < 4; ++j) x[j] = fmaxf(fmaxf(x[j], __uint_as_float(v[j][e])), __uint_as_float(v[j][e + 1]));
 #pragma unroll
             for (int j = 0; j < 4; ++j) top = fmaxf(top, fmaxf(x[j], __uint_as_float(v[j][31])));
-            top = top == -TQ_INF ? top : top * f;
+            top *= f;
           }
           const bool higher = top > m + kSlack;
           if (__any_sync(0xffffffffu, higher)) {
@@ -510,31 +512,28 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
           const float shift = m == -TQ_INF ? 0.f : kLift - m;
           const uint64_t f2 = both(f), shift2 = both(shift);
           uint64_t sum[2] = {0ull, 0ull};
+          auto weights = [&](auto is_edge) {
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            uint32_t p[16], pl[16];
+            for (int j = 0; j < 4; ++j) {
+              uint32_t p[16], pl[16];
 #pragma unroll
-            for (int e = 0; e < 32; e += 2) {
-              // -inf times f may be NaN where f is 0: masked scores stay out of the product
-              const bool out0 = edge && v[j][e] == 0xFF800000u, out1 = edge && v[j][e + 1] == 0xFF800000u;
-              fma2(v[j][e], v[j][e + 1], f2, shift2);
-              float x = ex2(__uint_as_float(v[j][e])), y = ex2(__uint_as_float(v[j][e + 1]));
-              if (edge) {
-                x = out0 ? 0.f : x;
-                y = out1 ? 0.f : y;
+              for (int e = 0; e < 32; e += 2) {
+                fma2(v[j][e], v[j][e + 1], f2, shift2);
+                float x = ex2(__uint_as_float(v[j][e])), y = ex2(__uint_as_float(v[j][e + 1]));
+                add2(sum[(e >> 1) & 1], x, y);
                 // values of a NaN block are zeros in the operand: the weight carries the NaN to the rows that see the block
-                if (((flags >> ((32 * j + e) >> 4)) & 1) && t0 + 32 * j + e < vis) x = __uint_as_float(0x7FC00000u);
+                if (decltype(is_edge)::value && ((flags >> ((32 * j + e) >> 4)) & 1) && t0 + 32 * j + e < vis) x = __uint_as_float(0x7FC00000u);
+                p[e >> 1] = pack2(x, y);
+                if (LIMBS == 2) {
+                  const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&p[e >> 1]));
+                  pl[e >> 1] = pack2(x - back.x, y - back.y);
+                }
               }
-              add2(sum[(e >> 1) & 1], x, y);
-              p[e >> 1] = pack2(x, y);
-              if (LIMBS == 2) {
-                const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&p[e >> 1]));
-                pl[e >> 1] = pack2(x - back.x, y - back.y);
-              }
+              tmem_st16(s_col + 16 * j, p);   // over columns of S that have been read
+              if (LIMBS == 2) tmem_st16(p_lo + 16 * j, pl);
             }
-            tmem_st16(s_col + 16 * j, p);   // over columns of S that have been read
-            if (LIMBS == 2) tmem_st16(p_lo + 16 * j, pl);
-          }
+          };
+          if (edge) weights(std::true_type{}); else weights(std::false_type{});
           l += sum_of(sum[0]) + sum_of(sum[1]);
           tc::tmem_st_wait();
           tc::tc_fence_before();

@@ -459,35 +459,41 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
           }
           const int t0 = (first + i) * kKeys, flags = sh.flags[nt & 3];
           const bool edge = t0 + kKeys > it.vis_min || flags != 0;
-          uint32_t v[4][32];
-          auto load_scores = [&] {
+          // S passes through the registers twice, 32 columns at a time with the next ones on their way: held whole it would spill
+          uint32_t v[2][32];
+          auto each = [&](auto&& f32) {     // f32(columns, which)
+            tc::tmem_ld32(s_col, v[0]);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) tc::tmem_ld32(s_col + 32 * j, v[j]);
-            tc::tmem_ld_wait();
+            for (int j = 0; j < 4; ++j) {
+              tc::tmem_ld_wait();
+              if (j < 3) tc::tmem_ld32(s_col + 32 * (j + 1), v[(j + 1) & 1]);
+              f32(v[j & 1], j);
+            }
           };
-          load_scores();
           // keys that the row does not see: -inf
-          auto mask = [&] {
+          auto mask = [&](uint32_t (&x)[32], int j) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-              for (int e = 0; e < 32; ++e)
-                if (t0 + 32 * j + e >= vis || ((flags >> (8 + ((32 * j + e) >> 4))) & 1)) v[j][e] = 0xFF800000u;
+            for (int e = 0; e < 32; ++e)
+              if (t0 + 32 * j + e >= vis || ((flags >> (8 + 2 * j + (e >> 4))) & 1)) x[e] = 0xFF800000u;
           };
-          if (edge) mask();
           float top = -TQ_INF;
-          {
-            float x[4];
+          auto largest = [&](auto is_edge) {
+            each([&](uint32_t (&x)[32], int j) {
+              if (decltype(is_edge)::value) mask(x, j);
+              float y[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) x[j] = __uint_as_float(v[j][0]);
+              for (int g = 0; g < 4; ++g) y[g] = __uint_as_float(x[8 * g]);
 #pragma unroll
-            for (int e = 1; e < 31; e += 2)
+              for (int e = 1; e < 7; e += 2)
 #pragma unroll
-              for (int j = 0; j < 4; ++j) x[j] = fmaxf(fmaxf(x[j], __uint_as_float(v[j][e])), __uint_as_float(v[j][e + 1]));
+                for (int g = 0; g < 4; ++g) y[g] = fmaxf(fmaxf(y[g], __uint_as_float(x[8 * g + e])), __uint_as_float(x[8 * g + e + 1]));
 #pragma unroll
-            for (int j = 0; j < 4; ++j) top = fmaxf(top, fmaxf(x[j], __uint_as_float(v[j][31])));
-            top *= f;
-          }
+              for (int g = 0; g < 4; ++g) y[g] = fmaxf(y[g], __uint_as_float(x[8 * g + 7]));
+              top = fmaxf(fmaxf(top, fmaxf(y[0], y[1])), fmaxf(y[2], y[3]));
+            });
+          };
+          if (edge) largest(std::true_type{}); else largest(std::false_type{});
+          top *= f;
           const bool higher = top > m + kSlack;
           if (__any_sync(0xffffffffu, higher)) {
             float alpha = 1.f;
@@ -505,24 +511,22 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
                 for (int e = 0; e < 32; ++e) v[0][e] = __float_as_uint(__uint_as_float(v[0][e]) * alpha);
                 tc::tmem_st32(o_col + 32 * j, v[0]);
               }
-              load_scores();                // S is still there, and registers are scarce
-              if (edge) mask();
             }
           }
           const float shift = m == -TQ_INF ? 0.f : kLift - m;
           const uint64_t f2 = both(f), shift2 = both(shift);
           uint64_t sum[2] = {0ull, 0ull};
           auto weights = [&](auto is_edge) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
+            each([&](uint32_t (&z)[32], int j) {
               uint32_t p[16], pl[16];
+              if (decltype(is_edge)::value) mask(z, j);
 #pragma unroll
               for (int e = 0; e < 32; e += 2) {
-                fma2(v[j][e], v[j][e + 1], f2, shift2);
-                float x = ex2(__uint_as_float(v[j][e])), y = ex2(__uint_as_float(v[j][e + 1]));
+                fma2(z[e], z[e + 1], f2, shift2);
+                float x = ex2(__uint_as_float(z[e])), y = ex2(__uint_as_float(z[e + 1]));
                 add2(sum[(e >> 1) & 1], x, y);
                 // values of a NaN block are zeros in the operand: the weight carries the NaN to the rows that see the block
-                if (decltype(is_edge)::value && ((flags >> ((32 * j + e) >> 4)) & 1) && t0 + 32 * j + e < vis) x = __uint_as_float(0x7FC00000u);
+                if (decltype(is_edge)::value && ((flags >> (2 * j + (e >> 4))) & 1) && t0 + 32 * j + e < vis) x = __uint_as_float(0x7FC00000u);
                 p[e >> 1] = pack2(x, y);
                 if (LIMBS == 2) {
                   const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&p[e >> 1]));
@@ -531,7 +535,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
               }
               tmem_st16(s_col + 16 * j, p);   // over columns of S that have been read
               if (LIMBS == 2) tmem_st16(p_lo + 16 * j, pl);
-            }
+            });
           };
           if (edge) weights(std::true_type{}); else weights(std::false_type{});
           l += sum_of(sum[0]) + sum_of(sum[1]);

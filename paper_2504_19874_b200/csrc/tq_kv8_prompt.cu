@@ -11,8 +11,8 @@
 // Work.  A CTA per SM; units are (tile of 128 keys) x (block of 256 rows, fp32: 128), numbered through over blocks, heads and sequences,
 // and every CTA takes an equal run of them, so that causal triangles and ragged batches are even; runs that end inside a block leave
 // parts that the join kernel adds up.
-// Warps: two groups of four for the softmax of a row tile each (a thread per row, no shuffles), three that expand codes from global memory
-// through registers into the operand layout, one that issues the MMAs.  While one group works on its S, the tensor cores work for the
+// Warps: two groups of four for the softmax of a row tile each (a thread per row, no shuffles), four and three that expand keys and values
+// from global memory through registers into the operand layout, one that issues the MMAs.  While one group works on its S, the tensor cores work for the
 // other.  Waits are bounded; a CTA that gives up writes NaN.
 #include <algorithm>
 #include <cstring>
@@ -26,7 +26,8 @@ namespace tq {
 namespace kv8 {
 namespace {
 
-constexpr int kExpandWarps = 3, kThreads = 384, kExpandWarp0 = 8, kMmaWarp = 11;   // three warps per scheduler: 168 registers each
+// Four warps per scheduler, 128 registers each: 8 for the softmax, 4 that expand keys, 3 that expand values, 1 for the MMAs.
+constexpr int kThreads = 512, kExpandWarp0 = 8, kKeyWarps = 4, kValueWarps = 3, kMmaWarp = 15;
 constexpr int kKeys = 128;                  // of a tile
 constexpr uint32_t kPanel = kKeys * 128;    // bytes of 128 rows x 64 fp16
 
@@ -298,9 +299,9 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
     tc::mbar_init(&sh.bar.o_done, 1);
     tc::mbar_init(&sh.bar.drain, 1);
     for (int i = 0; i < 2; ++i) {
-      tc::mbar_init(&sh.bar.k_full[i], 32 * kExpandWarps);
+      tc::mbar_init(&sh.bar.k_full[i], 32 * kKeyWarps);
       tc::mbar_init(&sh.bar.k_empty[i], 1);
-      tc::mbar_init(&sh.bar.v_full[i], 32 * kExpandWarps);
+      tc::mbar_init(&sh.bar.v_full[i], 32 * kValueWarps);
       tc::mbar_init(&sh.bar.v_empty[i], 1);
       tc::mbar_init(&sh.bar.s_ready[i], 1);
       tc::mbar_init(&sh.bar.p_ready[i], 128);
@@ -594,8 +595,12 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
       }
     } else if (warp >= kExpandWarp0 && warp < kMmaWarp) {
       // ================================================================ codes -> fp16 operands
-      const int we = warp - kExpandWarp0;   // takes keys 16 g .. 16 g + 15 of a tile for g = we, we + 3, we + 6
-      constexpr int G = (8 + kExpandWarps - 1) / kExpandWarps, N = D / 32;   // 16-byte chunks per lane of 16 keys
+      const bool isv = warp >= kExpandWarp0 + kKeyWarps;
+      // takes keys 16 g .. 16 g + 15 of a tile for g = we, we + stride, ..
+      const int we = warp - kExpandWarp0 - (isv ? kKeyWarps : 0), stride = isv ? kValueWarps : kKeyWarps;
+      constexpr int G = 3, N = D / 32;      // at most; 16-byte chunks per lane of 16 keys
+      uint64_t *full = isv ? sh.bar.v_full : sh.bar.k_full, *empty = isv ? sh.bar.v_empty : sh.bar.k_empty;
+      uint8_t* operand = isv ? v_sm : k_sm;
       while (u < u_end && ok) {
         const int n = min(u_end, item_at + it.tiles) - u, first = u - item_at;
         const int32_t* row_pages = a.b.table + (int64_t)it.b * a.b.ldt;
@@ -619,12 +624,12 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
             top_v = fmaxf(top_v, __shfl_xor_sync(0xffffffffu, top_v, o));
           }
         }
-        if (we == 0 && lane == 0) {
+        if (!isv && we == 0 && lane == 0) {
           sh.uk[n_item & 3] = top_k;
           sh.uv[n_item & 3] = top_v;
         }
-        const float inv_k = block_inverse(top_k), inv_v = block_inverse(top_v);
-        uint4 kr[G][N], vr[G][N];
+        const float inv = block_inverse(isv ? top_v : top_k);
+        uint4 raw[G][N];
         // what lane l < 8 knows of keys 16 l .. 16 l + 15 of a tile: page and scales; looked up two tiles ahead
         struct Known { int id; float ks, vs; };
         auto look_up = [&](int tile_no) -> Known {
@@ -641,11 +646,11 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
           return x;
         };
         const int64_t head_bytes = (int64_t)D << a.c.page_shift, page_bytes = head_bytes * a.c.heads;
-        const uint8_t *k_head = a.c.k + it.head * head_bytes, *v_head = a.c.v + it.head * head_bytes;
-        auto read = [&](const uint8_t* codes, int id8, int tile_no, uint4 (&x)[G][N]) {
+        const uint8_t* codes = (isv ? a.c.v : a.c.k) + it.head * head_bytes;
+        auto read = [&](int id8, int tile_no, uint4 (&x)[G][N]) {
 #pragma unroll
           for (int g = 0; g < G; ++g) {
-            const int grp = we + kExpandWarps * g, id = __shfl_sync(0xffffffffu, id8, grp & 7);
+            const int grp = we + stride * g, id = __shfl_sync(0xffffffffu, id8, grp & 7);
             const int t0 = tile_no * kKeys + 16 * grp;
             const uint8_t* from = codes + id * page_bytes + (t0 & ((1 << a.c.page_shift) - 1)) * D;
             if (grp < 8 && id >= 0 && t0 + 16 <= it.vis_max) {
@@ -666,13 +671,12 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
             }
           }
         };
-        auto write = [&](uint8_t* operand, const uint4 (&x)[G][N], float ratio, bool zero_nan) {
+        auto write = [&](uint8_t* base, const uint4 (&x)[G][N], float ratio) {
 #pragma unroll
           for (int g = 0; g < G; ++g) {
-            const int grp = we + kExpandWarps * g;
+            const int grp = we + stride * g;
             float r = __shfl_sync(0xffffffffu, ratio, grp & 7);
             if (grp >= 8) continue;
-            if (zero_nan && !(r == r)) r = 0.f;
             const __half2 r2 = __float2half2_rn(r), minus = __float2half2_rn(-1152.f * r);
 #pragma unroll
             for (int i = 0; i < N; ++i) {
@@ -682,7 +686,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
               uint32_t y[8];
 #pragma unroll
               for (int j = 0; j < 4; ++j) expand_scaled<E4M3>(w[j], r2, minus, y[2 * j], y[2 * j + 1]);
-              uint8_t* to = operand + (uint32_t)(chunk >> 2) * kPanel + (uint32_t)(16 * grp + row) * 128;
+              uint8_t* to = base + (uint32_t)(chunk >> 2) * kPanel + (uint32_t)(16 * grp + row) * 128;
               const int piece = (chunk & 3) * 2;
               *reinterpret_cast<uint4*>(to + ((piece ^ (row & 7)) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
               *reinterpret_cast<uint4*>(to + (((piece + 1) ^ (row & 7)) << 4)) = make_uint4(y[4], y[5], y[6], y[7]);
@@ -690,29 +694,22 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
           }
         };
         Known now = look_up(first), next = look_up(first + 1);
-        read(k_head, now.id, first, kr);
-        read(v_head, now.id, first, vr);
+        read(now.id, first, raw);
         for (int i = 0; i < n && ok; ++i) {
           const int nt = n_tile + i, st = nt & 1;
-          const uint32_t phase = ((nt >> 1) & 1) ^ 1;
-          const float rk = now.id >= 0 ? now.ks * inv_k : 0.f, rv = now.id >= 0 ? now.vs * inv_v : 0.f;
-          // slots of no page (those behind the last token are masked anyway), and NaN values
-          const uint32_t absent = __ballot_sync(0xffffffffu, lane < 8 && now.id < 0), nan = __ballot_sync(0xffffffffu, lane < 8 && !(rv == rv));
+          float r = now.id >= 0 ? (isv ? now.vs : now.ks) * inv : 0.f;
+          // slots of no page (those behind the last token are masked anyway), and NaN values, which become zeros: see the softmax
+          const uint32_t absent = __ballot_sync(0xffffffffu, lane < 8 && now.id < 0), nan = __ballot_sync(0xffffffffu, lane < 8 && !(now.vs == now.vs));
+          if (isv && !(r == r)) r = 0.f;
           now = next;
           next = look_up(first + i + 2);
-          ok = wait_all(&sh.bar.k_empty[st], phase);
+          ok = wait_all(&empty[st], ((nt >> 1) & 1) ^ 1);
           if (!ok) break;
-          if (we == 0 && lane == 0) sh.flags[nt & 3] = (int)(((absent & 0xFFu) << 8) | (nan & 0xFFu));
-          write(k_sm + st * OP, kr, rk, false);
+          if (!isv && we == 0 && lane == 0) sh.flags[nt & 3] = (int)(((absent & 0xFFu) << 8) | (nan & 0xFFu));
+          write(operand + st * OP, raw, r);
           tc::fence_proxy_async();
-          tc::mbar_arrive(&sh.bar.k_full[st]);
-          read(k_head, now.id, first + i + 1, kr);
-          ok = wait_all(&sh.bar.v_empty[st], phase);
-          if (!ok) break;
-          write(v_sm + st * OP, vr, rv, true);
-          tc::fence_proxy_async();
-          tc::mbar_arrive(&sh.bar.v_full[st]);
-          read(v_head, now.id, first + i + 1, vr);
+          tc::mbar_arrive(&full[st]);
+          read(now.id, first + i + 1, raw);
         }
         n_tile += n;
         ++n_item;

@@ -42,7 +42,7 @@ struct Shape {
 };
 
 struct Bars {
-  uint64_t q_ready, o_done, drain, k_full[2], k_empty[2], v_full[2], v_empty[2], s_ready[2], p_ready[2];
+  uint64_t q_ready, o_done, drain, k_full[2], k_empty[2], v_full[2], v_empty[2], s_ready[2][2], p_ready[2][2], tail[2];
 };
 struct Shared {
   Bars bar;
@@ -303,8 +303,11 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
       tc::mbar_init(&sh.bar.k_empty[i], 1);
       tc::mbar_init(&sh.bar.v_full[i], 32 * kValueWarps);
       tc::mbar_init(&sh.bar.v_empty[i], 1);
-      tc::mbar_init(&sh.bar.s_ready[i], 1);
-      tc::mbar_init(&sh.bar.p_ready[i], 128);
+      tc::mbar_init(&sh.bar.tail[i], 1);
+      for (int h = 0; h < 2; ++h) {
+        tc::mbar_init(&sh.bar.s_ready[i][h], 1);
+        tc::mbar_init(&sh.bar.p_ready[i][h], 128);
+      }
     }
     tc::fence_barrier_init();
   }
@@ -315,7 +318,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
   __syncthreads();
   tc::tc_fence_after();
   const uint32_t tmem = sh.tmem;
-  constexpr uint32_t O_COL = 256;           // S of the tiles at 0 and 128 (fp32: S, and P's low limb), O at 256 and 384
+  // S of row tile x and half h of the keys at 128 x + 64 h, P over its first 32 columns (fp32: the low limb 128 further on); O at 256 + 128 x
+  constexpr uint32_t O_COL = 256;
 
   // ---- this CTA's run of units
   int total = 0, before = 0, own = 0, upto = 0;
@@ -448,53 +452,45 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
         tc::fence_proxy_async();
         tc::mbar_arrive(&sh.bar.q_ready);
         float m = -TQ_INF, l = 0.f, uv = 0.f;
-        for (int i = 0; i < n && ok; ++i) {
-          const int nt = n_tile + i;
-          ok = wait_all(&sh.bar.s_ready[tile], nt & 1);
+        // Two halves of 64 keys take turns, so that the scores of one are there before the weights of the other are done.
+        for (int hi = 0; hi < 2 * n && ok; ++hi) {
+          const int nt = n_tile + (hi >> 1), half = hi & 1;
+          ok = wait_all(&sh.bar.s_ready[tile][half], nt & 1);
           if (!ok) break;
           tc::tc_fence_after();
-          if (i == 0) {                     // written before the item's first keys, which these scores have read
+          if (hi == 0) {                    // written before the item's first keys, which these scores have read
             f *= sh.uk[n_item & 3];
             if (f < 1e-30f) f = 1e-30f;     // keys of zeros, or no scale: all scores are (nearly) 0, and -inf stays what it is
             uv = sh.uv[n_item & 3];
           }
-          const int t0 = (first + i) * kKeys, flags = sh.flags[nt & 3];
-          const bool edge = t0 + kKeys > it.vis_min || flags != 0;
-          // S passes through the registers twice, 32 columns at a time with the next ones on their way: held whole it would spill
+          const int t0 = first * kKeys + hi * 64, flags = sh.flags[nt & 3] >> (4 * half);   // bits 0-3: NaN values, 8-11: no page
+          const bool edge = t0 + 64 > it.vis_min || (flags & 0xF0F) != 0;
+          const uint32_t s_half = s_col + 64 * half;
           uint32_t v[2][32];
-          auto each = [&](auto&& f32) {     // f32(columns, which)
-            tc::tmem_ld32(s_col, v[0]);
+          tc::tmem_ld32(s_half, v[0]);
+          tc::tmem_ld32(s_half + 32, v[1]);
+          tc::tmem_ld_wait();
+          if (edge) {                       // keys that the row does not see: -inf
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              tc::tmem_ld_wait();
-              if (j < 3) tc::tmem_ld32(s_col + 32 * (j + 1), v[(j + 1) & 1]);
-              f32(v[j & 1], j);
-            }
-          };
-          // keys that the row does not see: -inf
-          auto mask = [&](uint32_t (&x)[32], int j) {
+            for (int j = 0; j < 2; ++j)
 #pragma unroll
-            for (int e = 0; e < 32; ++e)
-              if (t0 + 32 * j + e >= vis || ((flags >> (8 + 2 * j + (e >> 4))) & 1)) x[e] = 0xFF800000u;
-          };
-          float top = -TQ_INF;
-          auto largest = [&](auto is_edge) {
-            each([&](uint32_t (&x)[32], int j) {
-              if (decltype(is_edge)::value) mask(x, j);
-              float y[4];
+              for (int e = 0; e < 32; ++e)
+                if (t0 + 32 * j + e >= vis || ((flags >> (8 + 2 * j + (e >> 4))) & 1)) v[j][e] = 0xFF800000u;
+          }
+          float top;
+          {
+            float x[4];
 #pragma unroll
-              for (int g = 0; g < 4; ++g) y[g] = __uint_as_float(x[8 * g]);
+            for (int g = 0; g < 4; ++g) x[g] = __uint_as_float(v[g >> 1][16 * (g & 1)]);
 #pragma unroll
-              for (int e = 1; e < 7; e += 2)
+            for (int e = 1; e < 15; e += 2)
 #pragma unroll
-                for (int g = 0; g < 4; ++g) y[g] = fmaxf(fmaxf(y[g], __uint_as_float(x[8 * g + e])), __uint_as_float(x[8 * g + e + 1]));
+              for (int g = 0; g < 4; ++g)
+                x[g] = fmaxf(fmaxf(x[g], __uint_as_float(v[g >> 1][16 * (g & 1) + e])), __uint_as_float(v[g >> 1][16 * (g & 1) + e + 1]));
 #pragma unroll
-              for (int g = 0; g < 4; ++g) y[g] = fmaxf(y[g], __uint_as_float(x[8 * g + 7]));
-              top = fmaxf(fmaxf(top, fmaxf(y[0], y[1])), fmaxf(y[2], y[3]));
-            });
-          };
-          if (edge) largest(std::true_type{}); else largest(std::false_type{});
-          top *= f;
+            for (int g = 0; g < 4; ++g) x[g] = fmaxf(x[g], __uint_as_float(v[g >> 1][16 * (g & 1) + 15]));
+            top = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])) * f;
+          }
           const bool higher = top > m + kSlack;
           if (__any_sync(0xffffffffu, higher)) {
             float alpha = 1.f;
@@ -503,14 +499,19 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
               m = top;
               l *= alpha;
             }
-            if (i > 0) {                    // O holds nothing before the first tile
+            if (hi > 0) {                   // O holds nothing before the first half
+              // O is at rest once the last half's weights have been multiplied: the scores of the next half were asked for after that
+              ok = hi + 1 < 2 * n ? wait_all(&sh.bar.s_ready[tile][half ^ 1], (nt + half) & 1) : wait_all(&sh.bar.tail[tile], n_item & 1);
+              if (!ok) break;
+              tc::tc_fence_after();
 #pragma unroll 1
-              for (int j = 0; j < D / 32; ++j) {
-                tc::tmem_ld32(o_col + 32 * j, v[0]);
+              for (int j = 0; j < D / 16; ++j) {
+                uint32_t w[16];
+                tc::tmem_ld16(o_col + 16 * j, w);
                 tc::tmem_ld_wait();
 #pragma unroll
-                for (int e = 0; e < 32; ++e) v[0][e] = __float_as_uint(__uint_as_float(v[0][e]) * alpha);
-                tc::tmem_st32(o_col + 32 * j, v[0]);
+                for (int e = 0; e < 16; ++e) w[e] = __float_as_uint(__uint_as_float(w[e]) * alpha);
+                tmem_st16(o_col + 16 * j, w);
               }
             }
           }
@@ -518,13 +519,13 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
           const uint64_t f2 = both(f), shift2 = both(shift);
           uint64_t sum[2] = {0ull, 0ull};
           auto weights = [&](auto is_edge) {
-            each([&](uint32_t (&z)[32], int j) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
               uint32_t p[16], pl[16];
-              if (decltype(is_edge)::value) mask(z, j);
 #pragma unroll
               for (int e = 0; e < 32; e += 2) {
-                fma2(z[e], z[e + 1], f2, shift2);
-                float x = ex2(__uint_as_float(z[e])), y = ex2(__uint_as_float(z[e + 1]));
+                fma2(v[j][e], v[j][e + 1], f2, shift2);
+                float x = ex2(__uint_as_float(v[j][e])), y = ex2(__uint_as_float(v[j][e + 1]));
                 add2(sum[(e >> 1) & 1], x, y);
                 // values of a NaN block are zeros in the operand: the weight carries the NaN to the rows that see the block
                 if (decltype(is_edge)::value && ((flags >> (2 * j + (e >> 4))) & 1) && t0 + 32 * j + e < vis) x = __uint_as_float(0x7FC00000u);
@@ -534,15 +535,15 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
                   pl[e >> 1] = pack2(x - back.x, y - back.y);
                 }
               }
-              tmem_st16(s_col + 16 * j, p);   // over columns of S that have been read
-              if (LIMBS == 2) tmem_st16(p_lo + 16 * j, pl);
-            });
+              tmem_st16(s_half + 16 * j, p);   // over scores that have been read
+              if (LIMBS == 2) tmem_st16(p_lo + 64 * half + 16 * j, pl);
+            }
           };
           if (edge) weights(std::true_type{}); else weights(std::false_type{});
           l += sum_of(sum[0]) + sum_of(sum[1]);
           tc::tmem_st_wait();
           tc::tc_fence_before();
-          tc::mbar_arrive(&sh.bar.p_ready[tile]);
+          tc::mbar_arrive(&sh.bar.p_ready[tile][half]);
         }
         if (ok) ok = wait_all(&sh.bar.o_done, n_item & 1);
         const bool good = ok;
@@ -719,24 +720,25 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
       }
     } else if (warp == kMmaWarp && lane == 0) {
       // ================================================================ MMAs
-      constexpr uint32_t id_s = idesc_f16(kKeys, false), id_o = idesc_f16(D, true);
+      constexpr uint32_t id_s = idesc_f16(64, false), id_o = idesc_f16(D, true);
       const uint32_t q_at = tc::smem_u32(q_sm), k_at = tc::smem_u32(k_sm), v_at = tc::smem_u32(v_sm);
-      auto scores = [&](int tile, int st) {
+      auto scores = [&](int tile, int half, int st) {
 #pragma unroll
         for (int x = 0; x < LIMBS; ++x)
 #pragma unroll
           for (int k = 0; k < D / 16; ++k) {
             const uint32_t off = (uint32_t)(k >> 2) * kPanel + (uint32_t)(k & 3) * 32;
-            tc::umma_bf16(tmem + 128 * tile, tc::smem_desc_sw128(q_at + (tile + x) * OP + off), tc::smem_desc_sw128(k_at + st * OP + off), id_s,
-                          (x | k) != 0 ? 1u : 0u);
+            tc::umma_bf16(tmem + 128 * tile + 64 * half, tc::smem_desc_sw128(q_at + (tile + x) * OP + off),
+                          tc::smem_desc_sw128(k_at + st * OP + 8192 * half + off), id_s, (x | k) != 0 ? 1u : 0u);
           }
+        tc::umma_commit(&sh.bar.s_ready[tile][half]);
       };
-      auto sums = [&](int tile, int st, bool fresh) {
+      auto sums = [&](int tile, int half, int st, bool fresh) {
 #pragma unroll
         for (int x = 0; x < LIMBS; ++x)
 #pragma unroll
-          for (int k = 0; k < kKeys / 16; ++k)
-            umma_f16_ts(tmem + O_COL + 128 * tile, tmem + 128 * (tile + x) + 8 * k, desc_values(v_at + st * OP + 2048 * k), id_o,
+          for (int k = 0; k < 4; ++k)
+            umma_f16_ts(tmem + O_COL + 128 * tile, tmem + 128 * (tile + x) + 64 * half + 8 * k, desc_values(v_at + st * OP + 8192 * half + 2048 * k), id_o,
                         !fresh || (x | k) != 0 ? 1u : 0u);
       };
       while (u < u_end && ok) {
@@ -746,27 +748,31 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
         if (!ok) break;
         tc::tc_fence_after();
 #pragma unroll
-        for (int tile = 0; tile < TILES; ++tile) {
-          scores(tile, n_tile & 1);
-          tc::umma_commit(&sh.bar.s_ready[tile]);
-        }
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+          for (int tile = 0; tile < TILES; ++tile) scores(tile, half, n_tile & 1);
         tc::umma_commit(&sh.bar.k_empty[n_tile & 1]);
         for (int i = 0; i < n && ok; ++i) {
           const int nt = n_tile + i, st = nt & 1;
 #pragma unroll
-          for (int tile = 0; tile < TILES; ++tile) {
-            ok = ok && tc::mbar_wait(&sh.bar.p_ready[tile], nt & 1, abort_flag, status);
-            if (tile == 0) ok = ok && tc::mbar_wait(&sh.bar.v_full[st], (nt >> 1) & 1, abort_flag, status);
-            if (!ok) break;
-            tc::tc_fence_after();
-            sums(tile, st, i == 0);
-            if (i + 1 < n) {
-              if (tile == 0) ok = tc::mbar_wait(&sh.bar.k_full[(nt + 1) & 1], ((nt + 1) >> 1) & 1, abort_flag, status);
+          for (int half = 0; half < 2; ++half) {
+#pragma unroll
+            for (int tile = 0; tile < TILES; ++tile) {
+              ok = ok && tc::mbar_wait(&sh.bar.p_ready[tile][half], nt & 1, abort_flag, status);
+              if (tile == 0 && half == 0) ok = ok && tc::mbar_wait(&sh.bar.v_full[st], (nt >> 1) & 1, abort_flag, status);
               if (!ok) break;
               tc::tc_fence_after();
-              scores(tile, (nt + 1) & 1);
-              tc::umma_commit(&sh.bar.s_ready[tile]);
+              sums(tile, half, st, i == 0 && half == 0);
+              if (i + 1 == n) {
+                if (half == 0) tc::umma_commit(&sh.bar.tail[tile]);
+                continue;
+              }
+              if (tile == 0 && half == 0) ok = tc::mbar_wait(&sh.bar.k_full[(nt + 1) & 1], ((nt + 1) >> 1) & 1, abort_flag, status);
+              if (!ok) break;
+              tc::tc_fence_after();
+              scores(tile, half, (nt + 1) & 1);
             }
+            if (!ok) break;
           }
           if (!ok) break;
           tc::umma_commit(&sh.bar.v_empty[st]);

@@ -689,7 +689,7 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
     for (int i = 0; i < 4; ++i) store_out<T>(out + i, sum == 0.f ? 0.f : v[i] / sum);
   }
   if (lane == 0 && a.lse) a.lse[row * ((int64_t)a.c.heads * g) + head] =
-      sum == 0.f ? -TQ_INF : (best == -TQ_INF ? 0.f : (best - kLift) * kLn2) + logf(sum);
+      sum == 0.f ? -TQ_INF : (best == -TQ_INF ? 0.f : (best - a.lift) * kLn2) + logf(sum);
 }
 
 template <typename T, int D, bool E4M3, int NT>
@@ -759,6 +759,7 @@ cudaError_t launch_attend(AttendArgs& a, int dtype, bool e4m3, int cols, int sms
   a.part_ml = reinterpret_cast<float*>(w + s.ml);
   a.part_o = reinterpret_cast<float*>(w + s.o);
   a.pitch = kMaxCols;
+  a.lift = kLift;
   const int nt = cols <= 8 ? 1 : 2;
   return dtype == TQ_F32 ? launch_t<float>(a, e4m3, nt, sms, st) : launch_t<__nv_bfloat16>(a, e4m3, nt, sms, st);
 }

@@ -8,7 +8,7 @@ namespace kv8 {
 
 constexpr int kMaxCols = 16;      // columns of a block of the few-query kernel
 constexpr int kPromptRows = 256;  // at most, of a block of the many-query kernel
-constexpr float kLift = 6.f;      // weights are 2^(score - maximum + kLift): more of the small ones are normal fp16 numbers
+constexpr float kLift = 6.f;      // (few-query kernel) weights are 2^(score - maximum + kLift): more of the small ones are normal fp16 numbers
 constexpr float kSlack = 8.f;     // a maximum only moves when a score exceeds it by this much (in powers of two)
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
@@ -32,6 +32,7 @@ struct AttendArgs {
   Meta* meta;             // workspace
   float *part_ml, *part_o;
   int pitch;              // columns of a part
+  float lift;             // of its weights
 };
 
 // The many-query kernel (tq_kv8_prompt.cu): workspace beside the few-query kernel's, and its launch, which is followed by the join.

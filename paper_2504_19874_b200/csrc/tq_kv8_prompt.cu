@@ -1,9 +1,9 @@
 // Attention over a paged 8-bit KV cache for many queries per sequence (prompts, chunks of prompts), on tcgen05.
 //
 // Mathematics.  Rows are (token, head of the group) pairs of one sequence and KV head; per tile of 128 rows and 128 keys
-//   S = Q K^T (TMEM),  p = 2^(s - m + 6) with the row's running maximum m,  O += P V (TMEM, P as the A operand from TMEM).
+//   S = Q K^T (TMEM),  p = 2^(s - m + lift) with the row's running maximum m,  O += P V (TMEM, P as the A operand from TMEM).
 // As in the few-query kernel queries are scaled per row by a power of two into [2^13, 2^14) and held in fp16 (fp32 ones as two limbs),
-// P is one fp16 limb for bf16 outputs and two for fp32 ones, and m moves only when a score exceeds it by 2^8: then the row's O in
+// P is one fp16 limb for bf16 outputs and two for fp32 ones, and m moves only when a score exceeds it by far: then the row's O in
 // TMEM is rescaled by its own thread.  All sums are fp32.
 // The codes become fp16 in shared memory, times their block's scale over the largest scale of the pages in hand (a power of two, so
 // exact down to 2^-24 of that scale, 2^-31 of the largest number): the one factor left per row goes into the softmax or the output.
@@ -38,21 +38,19 @@ struct Shape {
   static constexpr int kRows = 128 * kTiles;
   static constexpr int kPanels = (D + 63) / 64;
   static constexpr uint32_t kOperand = kPanels * kPanel;          // a tile of 128 rows: queries, keys or values
-  static constexpr uint32_t smem = 6 * kOperand + 1024 + 1024;    // two of queries (row tiles, or limbs), two stages of keys and values
+  static constexpr uint32_t smem = 6 * kOperand + 1024 + 2048;    // two of queries (row tiles, or limbs), two stages of keys and values
+};
+
+// Weights are 2^(s - m + kLift), and m moves when a score exceeds it by more than kSlack: rescaling O costs about as much as a tile.  fp32
+// outputs keep the few-query kernel's figures; for bf16 ones weights below 2^-17 of the largest may lose bits (2^-28 of it each).
+template <typename T>
+struct Range {
+  static constexpr float kLift = sizeof(T) == 4 ? 6.f : 3.f, kSlack = sizeof(T) == 4 ? 8.f : 11.f;
 };
 
 struct Bars {
-  uint64_t q_ready, o_done, drain, k_full[2], k_empty[2], v_full[2], v_empty[2], s_ready[2][2], p_ready[2][2], tail[2];
+  uint64_t q_ready, o_done, drain, k_full[2], k_empty[2], v_full[2], v_empty[2], s_ready[2], p_ready[2][2];
 };
-struct Shared {
-  Bars bar;
-  float uk[4], uv[4];                       // largest scales of the items in hand, by the item's number
-  int flags[4];                             // of tiles, by number: bits 0-7: 16 keys whose values are NaN; 8-15: 16 keys of no page
-  uint32_t tmem;
-  int abort_flag;
-  int sums[16], found[4];
-};
-
 // ---- work: full blocks of `rows` rows of a sequence see ever more keys; the sum over the first n of them in closed form
 __device__ __forceinline__ int64_t quot(int64_t a, int64_t b) {
   return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
@@ -124,6 +122,16 @@ struct Item {
   int vis_min, vis_max;  // keys that its first and its last column see
   Seq s;
 };
+struct Shared {
+  Bars bar;
+  float uk[4], uv[4];                       // largest scales of the items in hand, by the item's number
+  int flags[4];                             // of tiles, by number: bits 0-7: 16 keys whose values are NaN; 8-15: 16 keys of no page
+  uint32_t tmem;
+  int abort_flag;
+  int sums[16], found[4];
+  Item item[kThreads / 32];                 // what each warp is at: registers are for the scores
+};
+
 __device__ __forceinline__ void describe(const AttendArgs& a, int rows, Item* it) {
   it->row0 = it->s.begin;
   it->col0 = it->block * rows;
@@ -154,12 +162,17 @@ __device__ __forceinline__ void umma_f16_ts(uint32_t d, uint32_t a, uint64_t b, 
       ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
       : "memory");
 }
-__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[16]) {
+__device__ __forceinline__ void tmem_st(uint32_t taddr, const uint32_t (&v)[16]) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
       ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
         "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
       : "memory");
+}
+__device__ __forceinline__ void tmem_st(uint32_t taddr, const uint32_t (&v)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+               : "memory");
 }
 // Values as the B operand with n (channels) contiguous: rows of 64 channels per key with the 128-byte swizzle, groups of 8 keys 1,024
 // bytes apart, the next 64 channels one panel on.
@@ -216,7 +229,13 @@ __device__ __forceinline__ void row8(const T* p, bool vec, float (&x)[8]) {
     }
   }
 }
-// 32 consecutive results of a row.
+// Whole 32-byte sectors: a warp's rows lie apart, and halves of sectors would cost as much each.
+__device__ __forceinline__ void store_sector(void* p, const uint32_t (&w)[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+               : "memory");
+}
+// 32 consecutive results of a row; `vec`: the row is 32-byte aligned.
 template <typename T>
 __device__ __forceinline__ void store32(T* p, bool vec, const uint32_t (&v)[32], float by) {
   if (!vec) {
@@ -224,19 +243,22 @@ __device__ __forceinline__ void store32(T* p, bool vec, const uint32_t (&v)[32],
     for (int e = 0; e < 32; ++e) store_out<T>(p + e, __uint_as_float(v[e]) * by);
   } else if (sizeof(T) == 4) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-      reinterpret_cast<float4*>(p)[e] = make_float4(__uint_as_float(v[4 * e]) * by, __uint_as_float(v[4 * e + 1]) * by,
-                                                    __uint_as_float(v[4 * e + 2]) * by, __uint_as_float(v[4 * e + 3]) * by);
+    for (int e = 0; e < 4; ++e) {
+      uint32_t w[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) w[j] = __float_as_uint(__uint_as_float(v[8 * e + j]) * by);
+      store_sector(p + 8 * e, w);
+    }
   } else {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      uint32_t w[4];
+    for (int e = 0; e < 2; ++e) {
+      uint32_t w[8];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float(v[8 * e + 2 * j]) * by, __uint_as_float(v[8 * e + 2 * j + 1]) * by);
+      for (int j = 0; j < 8; ++j) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float(v[16 * e + 2 * j]) * by, __uint_as_float(v[16 * e + 2 * j + 1]) * by);
         w[j] = *reinterpret_cast<const uint32_t*>(&h);
       }
-      reinterpret_cast<uint4*>(p)[e] = make_uint4(w[0], w[1], w[2], w[3]);
+      store_sector(p + 16 * e, w);
     }
   }
 }
@@ -303,11 +325,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
       tc::mbar_init(&sh.bar.k_empty[i], 1);
       tc::mbar_init(&sh.bar.v_full[i], 32 * kValueWarps);
       tc::mbar_init(&sh.bar.v_empty[i], 1);
-      tc::mbar_init(&sh.bar.tail[i], 1);
-      for (int h = 0; h < 2; ++h) {
-        tc::mbar_init(&sh.bar.s_ready[i][h], 1);
-        tc::mbar_init(&sh.bar.p_ready[i][h], 128);
-      }
+      tc::mbar_init(&sh.bar.s_ready[i], 1);
+      for (int h = 0; h < 2; ++h) tc::mbar_init(&sh.bar.p_ready[i][h], 128);
     }
     tc::fence_barrier_init();
   }
@@ -318,7 +337,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
   __syncthreads();
   tc::tc_fence_after();
   const uint32_t tmem = sh.tmem;
-  // S of row tile x and half h of the keys at 128 x + 64 h, P over its first 32 columns (fp32: the low limb 128 further on); O at 256 + 128 x
+  // S of row tile x at 128 x, P over its first 64 columns (fp32: the low limb 128 further on); O at 256 + 128 x
   constexpr uint32_t O_COL = 256;
 
   // ---- this CTA's run of units
@@ -356,8 +375,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
   Meta* meta = a.meta + blockIdx.x;
   if (t == 0) meta->last_cta = -1;
   int item_at = 0;
-  Item it;
   if (u0 < u_end) {
+    Item& it = sh.item[warp];
 #pragma unroll 1
     for (int b0 = 0;; b0 += kThreads) {
       int all = total;
@@ -376,22 +395,25 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
       }
       before += all;
     }
-    it.b = sh.found[0];
-    it.s = seq_of(a, it.b, ROWS);
     {
-      const int of_head = tiles_before(a, it.s, ROWS, it.s.blocks), rest = u0 - sh.found[1];
-      it.head = rest / of_head;
-      const int at = rest - it.head * of_head;
-      int lo = 0, hi = it.s.blocks - 1;     // the last block whose first unit is not behind u0
+      Item start;
+      start.b = sh.found[0];
+      start.s = seq_of(a, start.b, ROWS);
+      const int of_head = tiles_before(a, start.s, ROWS, start.s.blocks), rest = u0 - sh.found[1];
+      start.head = rest / of_head;
+      const int at = rest - start.head * of_head;
+      int lo = 0, hi = start.s.blocks - 1;  // the last block whose first unit is not behind u0
 #pragma unroll 1
       while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
-        if (tiles_before(a, it.s, ROWS, mid) <= at) lo = mid; else hi = mid - 1;
+        if (tiles_before(a, start.s, ROWS, mid) <= at) lo = mid; else hi = mid - 1;
       }
-      it.block = lo;
-      item_at = u0 - at + tiles_before(a, it.s, ROWS, lo);
+      start.block = lo;
+      item_at = u0 - at + tiles_before(a, start.s, ROWS, lo);
+      describe(a, ROWS, &start);
+      if (lane == 0) it = start;
+      __syncwarp();
     }
-    describe(a, ROWS, &it);
 
     int u = u0;
     int n_item = 0, n_tile = 0;             // of this CTA, for phases and slots
@@ -418,7 +440,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
           const bool vec = (reinterpret_cast<uintptr_t>(q) & 15) == 0;
           uint32_t most = 0u;
           if (mine)
-#pragma unroll 4
+#pragma unroll 8
             for (int i = 0; i < D / 8; ++i) {
               float x[8];
               row8(q + 8 * i, vec, x);
@@ -430,7 +452,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
           // a negative scale goes into the queries: the largest sum is then the largest score
           f = most >= 0x7F800000u ? __uint_as_float(0x7FC00000u) : s * fabsf(a.scale * kLog2e);
           inv = a.scale < 0.f ? -inv : inv;
-#pragma unroll 4
+#pragma unroll 2
           for (int i = 0; i < D / 8; ++i) {
             float x[8];
 #pragma unroll
@@ -452,33 +474,32 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
         tc::fence_proxy_async();
         tc::mbar_arrive(&sh.bar.q_ready);
         float m = -TQ_INF, l = 0.f, uv = 0.f;
-        // Two halves of 64 keys take turns, so that the scores of one are there before the weights of the other are done.
-        for (int hi = 0; hi < 2 * n && ok; ++hi) {
-          const int nt = n_tile + (hi >> 1), half = hi & 1;
-          ok = wait_all(&sh.bar.s_ready[tile][half], nt & 1);
+        for (int i = 0; i < n && ok; ++i) {
+          const int nt = n_tile + i;
+          ok = wait_all(&sh.bar.s_ready[tile], nt & 1);
           if (!ok) break;
           tc::tc_fence_after();
-          if (hi == 0) {                    // written before the item's first keys, which these scores have read
+          if (i == 0) {                     // written before the item's first keys, which these scores have read
             f *= sh.uk[n_item & 3];
             if (f < 1e-30f) f = 1e-30f;     // keys of zeros, or no scale: all scores are (nearly) 0, and -inf stays what it is
             uv = sh.uv[n_item & 3];
           }
-          const int t0 = first * kKeys + hi * 64, flags = sh.flags[nt & 3] >> (4 * half);   // bits 0-3: NaN values, 8-11: no page
-          const bool edge = t0 + 64 > it.vis_min || (flags & 0xF0F) != 0;
-          const uint32_t s_half = s_col + 64 * half;
+          const int t0 = (first + i) * kKeys, flags = sh.flags[nt & 3];   // bits 0-7: NaN values, 8-15: no page
+          const bool edge = t0 + kKeys > it.vis_min || flags != 0;
           uint32_t v[2][32];
-          tc::tmem_ld32(s_half, v[0]);
-          tc::tmem_ld32(s_half + 32, v[1]);
-          tc::tmem_ld_wait();
-          if (edge) {                       // keys that the row does not see: -inf
+          auto load_half = [&](int half) {
+            tc::tmem_ld32(s_col + 64 * half, v[0]);
+            tc::tmem_ld32(s_col + 64 * half + 32, v[1]);
+            tc::tmem_ld_wait();
+            if (edge) {                     // keys that the row does not see: -inf
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
+              for (int j = 0; j < 2; ++j)
 #pragma unroll
-              for (int e = 0; e < 32; ++e)
-                if (t0 + 32 * j + e >= vis || ((flags >> (8 + 2 * j + (e >> 4))) & 1)) v[j][e] = 0xFF800000u;
-          }
-          float top;
-          {
+                for (int e = 0; e < 32; ++e)
+                  if (t0 + 64 * half + 32 * j + e >= vis || ((flags >> (8 + 4 * half + 2 * j + (e >> 4))) & 1)) v[j][e] = 0xFF800000u;
+            }
+          };
+          auto largest = [&]() -> float {
             float x[4];
 #pragma unroll
             for (int g = 0; g < 4; ++g) x[g] = __uint_as_float(v[g >> 1][16 * (g & 1)]);
@@ -489,9 +510,17 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
                 x[g] = fmaxf(fmaxf(x[g], __uint_as_float(v[g >> 1][16 * (g & 1) + e])), __uint_as_float(v[g >> 1][16 * (g & 1) + e + 1]));
 #pragma unroll
             for (int g = 0; g < 4; ++g) x[g] = fmaxf(x[g], __uint_as_float(v[g >> 1][16 * (g & 1) + 15]));
-            top = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])) * f;
+            return fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+          };
+          // Loops that are not unrolled keep the code of all roles small: instructions are fetched while operands wait (618 us against 688)
+          float top = -TQ_INF;
+#pragma unroll 1
+          for (int half = 1; half >= 0; --half) {   // the first half stays
+            load_half(half);
+            top = fmaxf(top, largest());
           }
-          const bool higher = top > m + kSlack;
+          top *= f;
+          const bool higher = top > m + Range<T>::kSlack;
           if (__any_sync(0xffffffffu, higher)) {
             float alpha = 1.f;
             if (higher) {
@@ -499,11 +528,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
               m = top;
               l *= alpha;
             }
-            if (hi > 0) {                   // O holds nothing before the first half
-              // O is at rest once the last half's weights have been multiplied: the scores of the next half were asked for after that
-              ok = hi + 1 < 2 * n ? wait_all(&sh.bar.s_ready[tile][half ^ 1], (nt + half) & 1) : wait_all(&sh.bar.tail[tile], n_item & 1);
-              if (!ok) break;
-              tc::tc_fence_after();
+            if (i > 0) {                    // O holds nothing before the first tile; it is at rest: these scores were asked for after its last sum
 #pragma unroll 1
               for (int j = 0; j < D / 16; ++j) {
                 uint32_t w[16];
@@ -511,39 +536,46 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
                 tc::tmem_ld_wait();
 #pragma unroll
                 for (int e = 0; e < 16; ++e) w[e] = __float_as_uint(__uint_as_float(w[e]) * alpha);
-                tmem_st16(o_col + 16 * j, w);
+                tmem_st(o_col + 16 * j, w);
               }
             }
           }
-          const float shift = m == -TQ_INF ? 0.f : kLift - m;
+          const float shift = m == -TQ_INF ? 0.f : Range<T>::kLift - m;
           const uint64_t f2 = both(f), shift2 = both(shift);
           uint64_t sum[2] = {0ull, 0ull};
-          auto weights = [&](auto is_edge) {
+          constexpr int W = LIMBS == 2 ? 16 : 32;   // keys per store: registers are scarce
+          auto weights = [&](auto is_edge, int half) {
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              uint32_t p[16], pl[16];
+            for (int g = 0; g < 64 / W; ++g) {
+              uint32_t p[W / 2], pl[W / 2];
 #pragma unroll
-              for (int e = 0; e < 32; e += 2) {
-                fma2(v[j][e], v[j][e + 1], f2, shift2);
-                float x = ex2(__uint_as_float(v[j][e])), y = ex2(__uint_as_float(v[j][e + 1]));
+              for (int e = 0; e < W; e += 2) {
+                const int key = W * g + e;
+                uint32_t &z0 = v[key >> 5][key & 31], &z1 = v[key >> 5][(key & 31) + 1];
+                fma2(z0, z1, f2, shift2);
+                float x = ex2(__uint_as_float(z0)), y = ex2(__uint_as_float(z1));
                 add2(sum[(e >> 1) & 1], x, y);
                 // values of a NaN block are zeros in the operand: the weight carries the NaN to the rows that see the block
-                if (decltype(is_edge)::value && ((flags >> (2 * j + (e >> 4))) & 1) && t0 + 32 * j + e < vis) x = __uint_as_float(0x7FC00000u);
+                if (decltype(is_edge)::value && ((flags >> (4 * half + (key >> 4))) & 1) && t0 + 64 * half + key < vis) x = __uint_as_float(0x7FC00000u);
                 p[e >> 1] = pack2(x, y);
                 if (LIMBS == 2) {
                   const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&p[e >> 1]));
                   pl[e >> 1] = pack2(x - back.x, y - back.y);
                 }
               }
-              tmem_st16(s_half + 16 * j, p);   // over scores that have been read
-              if (LIMBS == 2) tmem_st16(p_lo + 64 * half + 16 * j, pl);
+              tmem_st(s_col + 32 * half + W / 2 * g, p);   // over scores that have been read
+              if (LIMBS == 2) tmem_st(p_lo + 32 * half + W / 2 * g, pl);
             }
+            tc::tmem_st_wait();
+            tc::tc_fence_before();
+            tc::mbar_arrive(&sh.bar.p_ready[tile][half]);   // the first half is multiplied while the second is computed
           };
-          if (edge) weights(std::true_type{}); else weights(std::false_type{});
+#pragma unroll 1
+          for (int half = 0; half < 2; ++half) {
+            load_half(half);
+            if (edge) weights(std::true_type{}, half); else weights(std::false_type{}, half);
+          }
           l += sum_of(sum[0]) + sum_of(sum[1]);
-          tc::tmem_st_wait();
-          tc::tc_fence_before();
-          tc::mbar_arrive(&sh.bar.p_ready[tile][half]);
         }
         if (ok) ok = wait_all(&sh.bar.o_done, n_item & 1);
         const bool good = ok;
@@ -552,7 +584,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
         const int slot = 2 * (int)blockIdx.x + (u == item_at ? 1 : 0);
         const float by = !good ? __uint_as_float(0x7FC00000u) : (whole ? (l == 0.f ? 0.f : uv / l) : uv);
         T* out = static_cast<T*>(a.out) + q_row * a.ldo + (int64_t)q_head * a.ho;
-        const bool vec_out = (reinterpret_cast<uintptr_t>(out) & 15) == 0;
+        const bool vec_out = (reinterpret_cast<uintptr_t>(out) & 31) == 0;
         float* part = a.part_o + ((int64_t)slot * a.pitch + row) * D;
 #pragma unroll 1
         for (int j = 0; j < D / 32; ++j) {
@@ -577,7 +609,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
             a.part_ml[(int64_t)slot * 2 * a.pitch + a.pitch + row] = good ? l : by;
           } else if (a.lse) {
             a.lse[q_row * ((int64_t)a.c.heads * a.g) + q_head] =
-                !good ? by : (l == 0.f ? -TQ_INF : (m == -TQ_INF ? 0.f : (m - kLift) * kLn2) + logf(l));
+                !good ? by : (l == 0.f ? -TQ_INF : (m == -TQ_INF ? 0.f : (m - Range<T>::kLift) * kLn2) + logf(l));
           }
         }
         if (!whole && u == item_at && t == 0) {
@@ -592,7 +624,9 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
         ++n_item;
         u += n;
         item_at += it.tiles;
-        if (u < u_end) next_item(a, ROWS, &it);
+        __syncwarp();
+        if (lane == 0 && u < u_end) next_item(a, ROWS, &it);
+        __syncwarp();
       }
     } else if (warp >= kExpandWarp0 && warp < kMmaWarp) {
       // ================================================================ codes -> fp16 operands
@@ -716,29 +750,31 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
         ++n_item;
         u += n;
         item_at += it.tiles;
-        if (u < u_end) next_item(a, ROWS, &it);
+        __syncwarp();
+        if (lane == 0 && u < u_end) next_item(a, ROWS, &it);
+        __syncwarp();
       }
     } else if (warp == kMmaWarp && lane == 0) {
       // ================================================================ MMAs
-      constexpr uint32_t id_s = idesc_f16(64, false), id_o = idesc_f16(D, true);
+      constexpr uint32_t id_s = idesc_f16(kKeys, false), id_o = idesc_f16(D, true);
       const uint32_t q_at = tc::smem_u32(q_sm), k_at = tc::smem_u32(k_sm), v_at = tc::smem_u32(v_sm);
-      auto scores = [&](int tile, int half, int st) {
+      auto scores = [&](int tile, int st) {
 #pragma unroll
         for (int x = 0; x < LIMBS; ++x)
 #pragma unroll
           for (int k = 0; k < D / 16; ++k) {
             const uint32_t off = (uint32_t)(k >> 2) * kPanel + (uint32_t)(k & 3) * 32;
-            tc::umma_bf16(tmem + 128 * tile + 64 * half, tc::smem_desc_sw128(q_at + (tile + x) * OP + off),
-                          tc::smem_desc_sw128(k_at + st * OP + 8192 * half + off), id_s, (x | k) != 0 ? 1u : 0u);
+            tc::umma_bf16(tmem + 128 * tile, tc::smem_desc_sw128(q_at + (tile + x) * OP + off), tc::smem_desc_sw128(k_at + st * OP + off), id_s,
+                          (x | k) != 0 ? 1u : 0u);
           }
-        tc::umma_commit(&sh.bar.s_ready[tile][half]);
+        tc::umma_commit(&sh.bar.s_ready[tile]);
       };
       auto sums = [&](int tile, int half, int st, bool fresh) {
 #pragma unroll
         for (int x = 0; x < LIMBS; ++x)
 #pragma unroll
           for (int k = 0; k < 4; ++k)
-            umma_f16_ts(tmem + O_COL + 128 * tile, tmem + 128 * (tile + x) + 64 * half + 8 * k, desc_values(v_at + st * OP + 8192 * half + 2048 * k), id_o,
+            umma_f16_ts(tmem + O_COL + 128 * tile, tmem + 128 * (tile + x) + 32 * half + 8 * k, desc_values(v_at + st * OP + 8192 * half + 2048 * k), id_o,
                         !fresh || (x | k) != 0 ? 1u : 0u);
       };
       while (u < u_end && ok) {
@@ -748,31 +784,24 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
         if (!ok) break;
         tc::tc_fence_after();
 #pragma unroll
-        for (int half = 0; half < 2; ++half)
-#pragma unroll
-          for (int tile = 0; tile < TILES; ++tile) scores(tile, half, n_tile & 1);
+        for (int tile = 0; tile < TILES; ++tile) scores(tile, n_tile & 1);
         tc::umma_commit(&sh.bar.k_empty[n_tile & 1]);
         for (int i = 0; i < n && ok; ++i) {
           const int nt = n_tile + i, st = nt & 1;
 #pragma unroll
-          for (int half = 0; half < 2; ++half) {
-#pragma unroll
-            for (int tile = 0; tile < TILES; ++tile) {
-              ok = ok && tc::mbar_wait(&sh.bar.p_ready[tile][half], nt & 1, abort_flag, status);
-              if (tile == 0 && half == 0) ok = ok && tc::mbar_wait(&sh.bar.v_full[st], (nt >> 1) & 1, abort_flag, status);
-              if (!ok) break;
-              tc::tc_fence_after();
-              sums(tile, half, st, i == 0 && half == 0);
-              if (i + 1 == n) {
-                if (half == 0) tc::umma_commit(&sh.bar.tail[tile]);
-                continue;
-              }
-              if (tile == 0 && half == 0) ok = tc::mbar_wait(&sh.bar.k_full[(nt + 1) & 1], ((nt + 1) >> 1) & 1, abort_flag, status);
-              if (!ok) break;
-              tc::tc_fence_after();
-              scores(tile, half, (nt + 1) & 1);
-            }
+          for (int part = 0; part < 2 * TILES; ++part) {   // the groups are half a tile apart: 0 first half, 0 second, 1 first, 1 second
+            const int tile = part >> 1, half = part & 1;
+            ok = ok && tc::mbar_wait(&sh.bar.p_ready[tile][half], nt & 1, abort_flag, status);
+            if (part == 0) ok = ok && tc::mbar_wait(&sh.bar.v_full[st], (nt >> 1) & 1, abort_flag, status);
             if (!ok) break;
+            tc::tc_fence_after();
+            sums(tile, half, st, i == 0 && half == 0);
+            if (half == 1 && i + 1 < n) {
+              if (tile == 0) ok = tc::mbar_wait(&sh.bar.k_full[(nt + 1) & 1], ((nt + 1) >> 1) & 1, abort_flag, status);
+              if (!ok) break;
+              tc::tc_fence_after();
+              scores(tile, (nt + 1) & 1);
+            }
           }
           if (!ok) break;
           tc::umma_commit(&sh.bar.v_empty[st]);
@@ -839,6 +868,7 @@ cudaError_t launch_prompt(AttendArgs& a, int dtype, bool e4m3, int sms, void* wo
   a.part_ml = reinterpret_cast<float*>(w + s.ml);
   a.part_o = reinterpret_cast<float*>(w + s.o);
   a.pitch = kPromptRows;
+  a.lift = dtype == TQ_F32 ? Range<float>::kLift : Range<__nv_bfloat16>::kLift;
   int* status = reinterpret_cast<int*>(w + s.status);   // only written: a CTA whose wait ran out says so with NaN
   const cudaError_t e = dtype == TQ_F32 ? launch_t<float>(a, e4m3, status, sms, st) : launch_t<__nv_bfloat16>(a, e4m3, status, sms, st);
   if (e != cudaSuccess) return e;

@@ -98,8 +98,8 @@ def attend(pool, table, tokens, Q, scale, starts=None, lists=None):
     The tolerances count the roundings that the call documents.  A score is a sum of d products in fp32: off by at most
     (d + 16) 2^-24 of the sum of magnitudes, the 16 for the scaling of q (fp32: two fp16 limbs, 2^-22) and of the score; with it
     2^-22 |logit| for the exponent's argument and exp2.  A weight is then off by that relative amount twice (its own and the
-    sum's), and by its rounding to fp16 (2^-11) or to two limbs (2^-21); small weights are held to 2^-25 of 2^6 each (with a value scale up to 2^4 below the
-    largest one).  Sums of n weights: n 2^-24.  The output's own rounding: 2^-8 (bf16) or 2^-23."""
+    sum's), and by its rounding to fp16 (2^-11) or to two limbs (2^-21); small weights are held to 2^-25 of 2^3 (bf16) or 2^6 each, with a value scale up
+    to 2^4 below the largest one.  Sums of n weights: n 2^-24.  The output's own rounding: 2^-8 (bf16) or 2^-23."""
     n, hq, d = Q.shape
     T, heads = pool["k"].shape[2], pool["k"].shape[1]
     g = hq // heads
@@ -128,7 +128,7 @@ def attend(pool, table, tokens, Q, scale, starts=None, lists=None):
                 delta = ((d + 16) * 2.0 ** -24 * abs(scale) * (k.abs() @ q.abs()) + 2.0 ** -22 * logit.abs()).max()
                 tiny = k.shape[0] * 2.0 ** -31 * 16 * top
                 common = (2 * delta + k.shape[0] * 2.0 ** -24) * mag + 1e-37
-                tol16[r, j] = 2.0 ** -8 * out[r, j].abs() + 2.0 ** -11 * mag + tiny + common
+                tol16[r, j] = 2.0 ** -8 * out[r, j].abs() + 2.0 ** -11 * mag + 8 * tiny + common
                 tol32[r, j] = 2.0 ** -23 * out[r, j].abs() + 2.0 ** -21 * mag + tiny * 2.0 ** -11 + common
                 tol_l[r, j] = delta + k.shape[0] * 2.0 ** -24 + 2.0 ** -22 * (lse[r, j].abs() + 8)
     return out, lse, tol16, tol32, tol_l

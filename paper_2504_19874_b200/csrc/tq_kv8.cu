@@ -203,18 +203,47 @@ __global__ void __launch_bounds__(NT) append_kernel(const __grid_constant__ Appe
       reinterpret_cast<uint32_t*>(codes)[e] = o;
     }
   }
+  // A block that reads as NaN gets zeros.  Rounding keeps order, so the bounds of a channel's codes are the codes of its largest and
+  // smallest value: those are kept per thread where its vectors all hold the same channels.
+  const bool number = s1 == s1, aligned = NT % dv == 0;
+  float high[8], low[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    high[j] = -__uint_as_float(0x7F800000u);
+    low[j] = __uint_as_float(0x7F800000u);
+  }
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const int e = t + i * NT, slot = p0 + e / dv, ch = (e % dv) * 8;
     if (slot < p1) {
-      uint32_t o[2] = {0u, 0u};
+      float y[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const uint8_t c = encode<E4M3>(v[i][j] * inv);
-        o[j >> 2] |= (uint32_t)c << (8 * (j & 3));
-        if (bounds) bound(ch + j, c);
+        y[j] = number ? v[i][j] * inv : 0.f;
+        high[j] = fmaxf(high[j], y[j]);
+        low[j] = fminf(low[j], y[j]);
       }
-      *reinterpret_cast<uint2*>(codes + slot * d + ch) = make_uint2(o[0], o[1]);
+      const uint2 o = make_uint2(encode4<E4M3>(y[0], y[1], y[2], y[3]), encode4<E4M3>(y[4], y[5], y[6], y[7]));
+      *reinterpret_cast<uint2*>(codes + slot * d + ch) = o;
+      if (bounds && !aligned) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) bound(ch + j, (uint8_t)((j < 4 ? o.x : o.y) >> (8 * (j & 3))));
+      }
+    }
+  }
+  if (bounds && aligned) {
+    for (int x = dv; x < 32; x <<= 1)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        high[j] = fmaxf(high[j], __shfl_xor_sync(0xffffffffu, high[j], x));
+        low[j] = fminf(low[j], __shfl_xor_sync(0xffffffffu, low[j], x));
+      }
+    if (lane < dv && high[0] >= low[0]) {   // some row was here
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        bound((t % dv) * 8 + j, encode<E4M3>(high[j]));
+        bound((t % dv) * 8 + j, encode<E4M3>(low[j]));
+      }
     }
   }
   if (t == 0) *scale = s1;

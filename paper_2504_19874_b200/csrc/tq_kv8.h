@@ -105,6 +105,18 @@ __device__ __forceinline__ uint8_t encode(float x) {   // |x| <= 127 or 448; NaN
   if (E4M3) return (uint8_t)__nv_cvt_float_to_fp8(x, __NV_SATFINITE, __NV_E4M3);
   return (uint8_t)(int8_t)max(-127, min(127, __float2int_rn(x)));
 }
+// Four at a time, finite and in range.  int8: adding 1.5 * 2^23 rounds to the nearest even integer and leaves it in the low byte.
+template <bool E4M3>
+__device__ __forceinline__ uint32_t encode4(float a, float b, float c, float d) {
+  if (E4M3) {
+    const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
+    const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, __NV_E4M3);
+    return lo | (hi << 16);
+  }
+  const uint32_t x = __byte_perm(__float_as_uint(a + 12582912.f), __float_as_uint(b + 12582912.f), 0x0040);
+  const uint32_t y = __byte_perm(__float_as_uint(c + 12582912.f), __float_as_uint(d + 12582912.f), 0x0040);
+  return __byte_perm(x, y, 0x5410);
+}
 template <bool E4M3>
 __device__ __forceinline__ float decode(uint8_t c) {
   if (E4M3) return __half2float(__half(__nv_cvt_fp8_to_halfraw(c, __NV_E4M3)));

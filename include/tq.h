@@ -451,7 +451,7 @@ int tq_kv8_append(const tq_kv8* cache, const int32_t* table, int64_t ldt, int wi
  *   Q, out       [n rows, heads * q_per_kv, d] of dtype, row strides ldq / ldo, head strides hq / ho; 1 <= q_per_kv <= 256.
  *                TQ_BF16: weights are rounded to 11 bits; TQ_F32: products as exact as fp32 sums
  *   max_queries  no sequence has more rows than this
- *   lists        NULL, or [n, heads, nlist] int32: the numbers of the pages (entries of the sequence's row of the table) that a row
+ *   lists        NULL, or [n, heads, nlist >= 1] int32: the numbers of the pages (entries of the sequence's row of the table) that a row
  *                attends to, shared by the heads of a group, in any order; entries outside the sequence's pages are passed over, a
  *                page that is listed twice counts twice
  *   lse          [n, heads * q_per_kv] floats, or NULL
@@ -468,7 +468,7 @@ int tq_kv8_attend(const tq_kv8* cache, const int32_t* table, int64_t ldt, int wi
  *     score(page) = max over the group's heads of 2^e u s sum_c (max(qi_c, 0) B+_c + min(qi_c, 0) B-_c),
  * for scale > 0 no less than any logit of the page up to q's rounding.  Sums of integers and powers of two: scores are exact, and of
  * equal ones the lower page number is taken.  The first `first` and the last `last` pages that the row sees are always taken
- * (first + last <= k), and so is a block with scale NaN.  A query with an infinity or a NaN scores 0 everywhere.
+ * (first + last <= k), and so, as far as k goes, is a block with scale NaN.  A query with an infinity or a NaN scores 0 everywhere.
  *   lists      device out, [n, heads, k];  workspace  256-byte aligned, >= tq_kv8_select_workspace_bytes(cache, n, width)
  */
 size_t tq_kv8_select_workspace_bytes(const tq_kv8* cache, int64_t n, int width);

@@ -429,8 +429,8 @@ TQ_FN(kv8_append, 6) {   // cache, table, tokens, starts, K, V
 // [n, heads, k] contiguous int32
 int32_t* page_lists(PyObject* o, int64_t n, int heads, int* k) {
   const at::Tensor& t = on_device(o);
-  if (t.scalar_type() != at::kInt || t.dim() != 3 || t.size(0) != n || t.size(1) != heads || !t.is_contiguous() || t.size(2) > INT32_MAX)
-    fail("lists must be a contiguous int32 tensor [rows, KV heads, pages]");
+  if (t.scalar_type() != at::kInt || t.dim() != 3 || t.size(0) != n || t.size(1) != heads || !t.is_contiguous() || t.size(2) < 1 || t.size(2) > INT32_MAX)
+    fail("lists must be a contiguous int32 tensor [rows, KV heads, at least one page]");
   *k = (int)t.size(2);
   return t.data_ptr<int32_t>();
 }

@@ -591,7 +591,10 @@ cudaError_t launch_score(const SelectArgs& a, dim3 grid, size_t smem, cudaStream
   }
 }
 
-constexpr int64_t kRowsPerLaunch = 32768;
+// Rows that are scored before the next ones: as many as leave the keys within 64 MB, so that many rows need no workspace of their own.
+int64_t rows_per_launch(int heads, int width) {
+  return std::max<int64_t>(1, std::min<int64_t>(32768, (int64_t)(64 << 20) / ((int64_t)heads * width * (int64_t)sizeof(uint32_t))));
+}
 
 }  // namespace
 }  // namespace kv8
@@ -634,7 +637,7 @@ extern "C" int tq_kv8_append(const tq_kv8* cache, const int32_t* table, int64_t 
 
 extern "C" size_t tq_kv8_select_workspace_bytes(const tq_kv8* cache, int64_t n, int width) {
   if (cache == nullptr || n <= 0 || width <= 0 || cache->heads <= 0) return 0;
-  return (size_t)std::min<int64_t>(n, tq::kv8::kRowsPerLaunch) * cache->heads * width * sizeof(uint32_t);
+  return (size_t)std::min<int64_t>(n, tq::kv8::rows_per_launch(cache->heads, width)) * cache->heads * width * sizeof(uint32_t);
 }
 
 extern "C" int tq_kv8_select(const tq_kv8* cache, const int32_t* table, int64_t ldt, int width, int nseq, const int32_t* tokens,
@@ -682,8 +685,9 @@ extern "C" int tq_kv8_select(const tq_kv8* cache, const int32_t* table, int64_t 
     const int at = (dtype == TQ_F32 ? 0 : 4) + a.c.d / 32 - 1;
     TQ_CHECK_CUDA(allow_largest_smem(kern[at], devices[at]), who);
   }
-  for (int64_t row0 = 0; row0 < n; row0 += kRowsPerLaunch) {
-    const int64_t rows = std::min(kRowsPerLaunch, n - row0);
+  const int64_t most = width > 0 ? rows_per_launch(cache->heads, width) : 32768;
+  for (int64_t row0 = 0; row0 < n; row0 += most) {
+    const int64_t rows = std::min(most, n - row0);
     a.row0 = row0;
     if (width > k) {   // else every page is taken
       // a CTA's queries are quantised once for `per` pages: as many as leave eight CTAs per SM

@@ -794,7 +794,7 @@ extern "C" int tq_kv8_attend(const tq_kv8* cache, const int32_t* table, int64_t 
   TQ_REQUIRE(q_per_kv >= 1 && q_per_kv <= 256, TQ_ERR_UNSUPPORTED, "%s: 1..256 queries per KV head", who);
   TQ_REQUIRE(max_queries >= 0 && nlist >= 0, TQ_ERR_INVALID_ARG, "%s: negative size", who);
   TQ_REQUIRE(starts != nullptr || max_queries >= 1, TQ_ERR_INVALID_ARG, "%s: max_queries is 0 where every sequence has one row", who);
-  TQ_REQUIRE(lists != nullptr || nlist == 0, TQ_ERR_INVALID_ARG, "%s: lists is NULL", who);
+  TQ_REQUIRE((lists != nullptr) == (nlist > 0), TQ_ERR_INVALID_ARG, "%s: lists of %d pages", who, nlist);
   TQ_REQUIRE(nlist <= (1 << 24), TQ_ERR_UNSUPPORTED, "%s: lists of %d pages", who, nlist);
   if (nseq == 0 || n == 0 || max_queries == 0) return TQ_OK;
   TQ_REQUIRE(Q != nullptr && out != nullptr, TQ_ERR_INVALID_ARG, "%s: Q or out is NULL", who);

@@ -294,6 +294,53 @@ def test_attend_lists_of_any_kind():
     check_attend(bt, bt.randn(8, 6, torch.bfloat16), 0.4, starts, max_queries=3, lists=lists)
 
 
+def test_select_of_many_rows_takes_several_launches():
+    """Keys of 64 MB at a time: 300 rows of one head and 65,536 pages are scored in two goes."""
+    width, pages = 65536, 40
+    g = torch.Generator().manual_seed(3)
+    pool = {"k": torch.zeros((pages, 1, 16, 32), dtype=I8), "v": torch.zeros((pages, 1, 16, 32), dtype=I8), "k_scale": torch.ones((pages, 1)),
+            "v_scale": torch.ones((pages, 1)), "k_bounds": torch.randint(-100, 100, (pages, 1, 2, 32), generator=g, dtype=torch.int16).to(I8)}
+    table = torch.full((2, width), -1, dtype=torch.int32)
+    table[:, :pages] = torch.randperm(pages, generator=g).to(torch.int32)
+    tokens = torch.tensor([16 * 30, 16 * pages - 3], dtype=torch.int32)
+    starts = torch.tensor([0, 140, 300], dtype=torch.int32)
+    Q = torch.randn((300, 1, 32), generator=g)
+    cache = tq.Kv8Cache(*(pool[x].to(DEV) for x in ("k", "v", "k_scale", "v_scale", "k_bounds")))
+    nbytes = tq.tq_kv8_select_workspace_bytes(cache, 300, width)
+    assert nbytes < 300 * width * 4
+    lists = torch.full((300, 1, 7), -2, dtype=torch.int32, device=DEV)
+    tq.tq_kv8_select(cache, table.to(DEV), tokens.to(DEV), Q.to(DEV), lists, workspace(nbytes), starts=starts.to(DEV))
+    assert torch.equal(lists.cpu(), ref.select(pool, table[:, :pages], tokens, Q, 7, starts=starts))
+
+
+def test_offsets_past_32_bits():
+    """A pool whose keys alone take 5 GB, with the pages in use at its end."""
+    pages, page, d = 310_000, 128, 128
+    new = lambda *shape, dtype=I8: torch.empty(shape, dtype=dtype, device=DEV)
+    cache = tq.Kv8Cache(new(pages, 1, page, d), new(pages, 1, page, d), new(pages, 1, dtype=torch.float32), new(pages, 1, dtype=torch.float32),
+                        new(pages, 1, 2, d))
+    bt = Batch([400, 130], heads=1, d=d, page=page, seed=21, extra=0)
+    top = pages - 6
+    for name in ("k", "v", "k_scale", "v_scale", "k_bounds"):
+        getattr(cache, name)[top:].view(torch.uint8).copy_(bt.pool[name].view(torch.uint8).to(DEV))
+    bt.cache, bt.t, bt.n = cache, (bt.table + top).masked_fill(bt.table < 0, -1).to(DEV), bt.tokens.to(DEV)
+    check_attend(bt, bt.randn(2, 4, torch.bfloat16), 0.1)
+    starts = torch.tensor([0, 30, 60], dtype=torch.int32)
+    check_attend(bt, bt.randn(60, 4, torch.bfloat16), 0.1, starts, max_queries=30)
+    lists = torch.zeros((2, 1, 2), dtype=torch.int32, device=DEV)
+    Q = bt.randn(2, 4)
+    tq.tq_kv8_select(cache, bt.t, bt.n, Q.to(DEV), lists, workspace(tq.tq_kv8_select_workspace_bytes(cache, 2, bt.table.shape[1])))
+    assert torch.equal(lists.cpu(), ref.select(bt.pool, bt.table, bt.tokens, Q, 2))
+    K, V = bt.randn(2, 1), bt.randn(2, 1)
+    tq.tq_kv8_append(cache, bt.t, bt.n, K.to(DEV), V.to(DEV))
+    ref.append(bt.pool, bt.table, bt.tokens, K, V)
+    tq.tq_pages_copy(cache, torch.arange(top, pages, dtype=torch.int32, device=DEV), torch.arange(0, 6, dtype=torch.int32, device=DEV))
+    for name in ("k", "v", "k_scale", "v_scale", "k_bounds"):
+        want = torch.nan_to_num(bt.pool[name].float(), nan=-3.0)
+        for got in (getattr(cache, name)[top:], getattr(cache, name)[:6]):
+            assert torch.equal(torch.nan_to_num(got.cpu().float(), nan=-3.0), want), name
+
+
 # ---------------------------------------------------------------------------------------------------------------- used together
 
 @pytest.mark.parametrize("dtype", [I8, E4M3])

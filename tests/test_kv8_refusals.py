@@ -75,7 +75,7 @@ def test_append():
 def test_attend():
     c = cache()
     assert attend(c, g=0) == UNSUPPORTED and attend(c, g=257) == UNSUPPORTED
-    assert attend(c, max_queries=-1) == INVALID and attend(c, nlist=3) == INVALID and attend(c, lists=A, nlist=-1) == INVALID
+    assert attend(c, max_queries=-1) == INVALID and attend(c, nlist=3) == INVALID and attend(c, lists=A, nlist=-1) == INVALID and attend(c, lists=A, nlist=0) == INVALID
     assert attend(c, starts=None, n=2, max_queries=0) == INVALID
     assert attend(c, Q=None) == INVALID and attend(c, out=None) == INVALID
     assert attend(c, ldo=-1) == INVALID

@@ -107,8 +107,9 @@ __device__ __forceinline__ void find_slot(const AppendArgs& a, int64_t slot, int
 
 // One CTA quantises the new tokens of one page and head, keys (blockIdx.z = 0) or values (1): it alone knows the block's largest
 // magnitude, and old codes of the page are requantised where the scale grows.  NV vectors of 8 channels per thread hold what is new,
-// so the input is read once.  Bound by the input's bytes for prompts and by the chain of dependent loads (length, table, scale) for
-// single tokens.
+// so the input is read once.  A page per CTA, and not a row: the scale of the page needs all of its new rows at once.  Prompts are bound
+// by the input's bytes behind each CTA's chain of dependent loads (lengths, table, rows): 109 MB in 30 us, 3.6 TB/s; one token each of
+// 128 sequences by that chain alone, 4.4 us.
 template <typename T, bool E4M3, int NV, int NT>
 __global__ void __launch_bounds__(NT) append_kernel(const __grid_constant__ AppendArgs a) {
   __shared__ int found_seq;
@@ -294,7 +295,7 @@ constexpr int kScoreWarps = 4;
 // score(page) = max over the group's heads j of 2^e_j s unit sum_c (max(qi, 0) B+ + min(qi, 0) B-): an integer product over 2 d bytes,
 // so 16 pages x 8 heads x 32 bytes go into one mma with exact int32 sums, and the scores are exact in fp32 (an integer below 2^22
 // times powers of two).  A warp takes 16 pages at a time; a lane reads 16 bytes of a page's bounds, in an order of k that the queries
-// share.  Bound by the bounds' bytes, 2 d per page and head.
+// share.  Bound by the bounds' bytes, 2 d per page and head, and for few rows by latency: 2,048 pages of 8 heads (4 MB) in 4 us.
 template <typename T, int D>
 __global__ void __launch_bounds__(kScoreWarps * 32) score_kernel(const __grid_constant__ SelectArgs a) {
   constexpr int SEG = D / 32;              // 64-byte pieces of a page's bounds

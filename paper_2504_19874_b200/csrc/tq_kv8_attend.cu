@@ -629,54 +629,54 @@ __global__ void __launch_bounds__(kThreads, Kernel<T, D, E4M3, NT>::kCtas) atten
   }
 }
 
-// Joins the parts of the item that began in CTA blockIdx.x's share, in a fixed order: eight columns per blockIdx.y.  The warps of a column
-// take its parts in turn, and what the first parts hold is asked for before it is known how many there are (slots behind the last part
-// are read, never used).  Latency: 2 to 3 us behind the kernel that wrote the parts, whose end it waits for.
-constexpr int kJoinThreads = 512, kJoinWarps = kJoinThreads / 32, kJoinParts = 8;
+// Joins the parts of the item that began in CTA blockIdx.x's share, in a fixed order: eight columns per blockIdx.y, whose warps take a
+// column's parts in turn.  What the first parts hold is asked for before it is known how many there are (places behind the last part
+// are read, never used).  CTAs of 256 threads: most find nothing to do, and 512 threads each cost a ragged batch 3 us of 119; fewer CTAs that
+// look after several shares cost short calls 2.
+constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32, kJoinParts = 8;
 template <typename T, int D>
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ AttendArgs a, int c2) {   // c2: 1, 2, 4 or 8 columns at most
   __shared__ float4 o_s[kJoinWarps][32];
   wait_for_predecessor();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, first = blockIdx.x, ctas = gridDim.x;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, first = blockIdx.x;
   const int runs = kJoinWarps / c2, j = 8 * blockIdx.y + warp % c2, run = warp / c2;
-  auto slot = [&](int i) { return 2 * min(first + i, ctas - 1) + (i == 0 ? 1 : 0); };   // parts behind the last one are not used
   const float* po = a.part_o + (int64_t)j * D + 4 * min(lane, D / 4 - 1);
-  const Meta z = a.meta[first];
+  auto slot = [&](int i) { return 2 * min(first + i, (int)gridDim.x - 1) + (i == 0 ? 1 : 0); };
   float4 v[kJoinParts];
   auto fetch = [&](int i0) {
 #pragma unroll
     for (int i = 0; i < kJoinParts; ++i) v[i] = *reinterpret_cast<const float4*>(po + (int64_t)slot(i0 + i * runs) * a.pitch * D);
   };
-  float ml_m = a.part_ml[(int64_t)slot(lane) * 2 * a.pitch + j], ml_l = a.part_ml[(int64_t)slot(lane) * 2 * a.pitch + a.pitch + j];
+  const Meta z = a.meta[first];
+  const float* ml = a.part_ml + j;
+  const float m0 = ml[(int64_t)slot(lane) * 2 * a.pitch], l0 = ml[(int64_t)slot(lane) * 2 * a.pitch + a.pitch];
   fetch(run);
   const int cols = min(z.cols - 8 * (int)blockIdx.y, 8), parts = z.last_cta - first + 1;
   if (z.last_cta < 0 || cols <= 0) return;
   const bool mine = j - 8 * (int)blockIdx.y < cols;
-  float best = lane < parts ? ml_m : -TQ_INF;
-  for (int i = lane + 32; i < parts; i += 32) best = fmaxf(best, a.part_ml[(int64_t)slot(i) * 2 * a.pitch + j]);
+  float best = lane < parts ? m0 : -TQ_INF;
+  for (int i = lane + 32; i < parts; i += 32) best = fmaxf(best, ml[(int64_t)slot(i) * 2 * a.pitch]);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, o));
   float sum = 0.f;
   float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 1
   for (int p0 = 0; p0 < parts; p0 += 32) {   // weights of 32 parts, one per lane
-    if (p0 > 0) {
-      ml_m = a.part_ml[(int64_t)slot(p0 + lane) * 2 * a.pitch + j];
-      ml_l = a.part_ml[(int64_t)slot(p0 + lane) * 2 * a.pitch + a.pitch + j];
-    }
     float w = 0.f;
     if (p0 + lane < parts) {
-      w = best == -TQ_INF ? 1.f : ex2(ml_m - best);
-      sum += ml_l * w;
+      const int64_t at = (int64_t)slot(p0 + lane) * 2 * a.pitch;
+      w = best == -TQ_INF ? 1.f : ex2((p0 == 0 ? m0 : ml[at]) - best);
+      sum += (p0 == 0 ? l0 : ml[at + a.pitch]) * w;
     }
+    const int end = min(p0 + 32, parts);
 #pragma unroll 1
-    for (int i0 = p0 + run; i0 < min(p0 + 32, parts); i0 += kJoinParts * runs) {
+    for (int i0 = p0 + run; i0 < end; i0 += kJoinParts * runs) {
       if (i0 != run) fetch(i0);
 #pragma unroll
       for (int i = 0; i < kJoinParts; ++i) {
         const int at = i0 + i * runs;
         const float wi = __shfl_sync(0xffffffffu, w, (at - p0) & 31);
-        if (at < min(p0 + 32, parts)) {      // what is behind the last part may not be a number
+        if (at < end) {                      // what is behind may not be a number
           y.x = fmaf(v[i].x, wi, y.x); y.y = fmaf(v[i].y, wi, y.y); y.z = fmaf(v[i].z, wi, y.z); y.w = fmaf(v[i].w, wi, y.w);
         }
       }
@@ -757,8 +757,8 @@ static cudaError_t join_t(const AttendArgs& a, dim3 grid, int c2, cudaStream_t s
     default: return launch_dependent(join_kernel<T, 128>, grid, dim3(kJoinThreads), 0, st, a, c2);
   }
 }
-cudaError_t launch_join(const AttendArgs& a, int dtype, int grid, int cols, cudaStream_t st) {
-  const dim3 g((unsigned)grid, (unsigned)((cols + 7) / 8));
+cudaError_t launch_join(const AttendArgs& a, int dtype, int ctas, int cols, cudaStream_t st) {
+  const dim3 g((unsigned)ctas, (unsigned)((cols + 7) / 8));
   const int c2 = cols > 4 ? 8 : (cols > 2 ? 4 : cols);
   return dtype == TQ_F32 ? join_t<float>(a, g, c2, st) : join_t<__nv_bfloat16>(a, g, c2, st);
 }

@@ -38,7 +38,7 @@ struct AttendArgs {
 // The many-query kernel (tq_kv8_prompt.cu): workspace beside the few-query kernel's, and its launch, which is followed by the join.
 size_t prompt_space(int sms, int d);
 cudaError_t launch_prompt(AttendArgs& a, int dtype, bool e4m3, int sms, void* workspace, cudaStream_t st);
-cudaError_t launch_join(const AttendArgs& a, int dtype, int grid, int cols, cudaStream_t st);   // cols: of an item, at most
+cudaError_t launch_join(const AttendArgs& a, int dtype, int ctas, int cols, cudaStream_t st);   // ctas: shares; cols: of an item, at most
 
 #ifdef __CUDACC__
 #define TQ_INF __uint_as_float(0x7F800000u)

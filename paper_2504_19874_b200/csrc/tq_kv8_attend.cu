@@ -14,11 +14,11 @@
 // and of a unit each of its four warps takes 16 tokens, through a ring of its own in shared memory, some steps ahead.  Warps are
 // independent until their share of an item ends; items that several CTAs share are joined by a second, dependent launch in a fixed order.
 //
-// Measured, one B200, 8 KV heads x 4 queries, d = 128: 37 sequences of 8,192 tokens stream at 5.0 TB/s, a ragged batch of 64 (560 MB) at
-// 4.7 TB/s (119 us; 0.72 of the copy bandwidth), one sequence of 32,768 tokens 27 us, of which the loop takes 10 us at the copy bandwidth
-// and the chain of first loads, the last sums and the join the rest; 1,000 tokens 9.5 us.  Reading the tiles straight into registers,
-// one step ahead, took 228 us for the batch and 43 us for the layer: eight warps per SM had too few bytes on their way.  What bounds the
-// long calls is the dependent issue of 12 warps per SM (half of the slots; the ALU pipe, which unpacks the codes, half busy).
+// Measured, one B200, 8 KV heads x 4 queries, d = 128: 37 sequences of 8,192 tokens stream at 5.0 TB/s, a ragged batch of 64 (563 MB) at
+// 4.9 TB/s (115 us; 0.75 of the copy bandwidth), one sequence of 32,768 tokens 27 us, of which the loop takes 10 us at the copy bandwidth
+// and the chain of first loads, the last sums and the join the rest; 1,000 tokens 9.0 us.  Reading the tiles straight into registers,
+// one step ahead, took 228 us for the batch and 43 us for the layer: eight warps per SM had too few bytes on their way.  Long calls
+// are bound by HBM; half of the issue slots and of the ALU pipe, which unpacks the codes, are in use meanwhile.
 #include <algorithm>
 #include <cstring>
 

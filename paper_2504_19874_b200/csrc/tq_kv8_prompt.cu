@@ -15,8 +15,8 @@
 // from global memory through registers into the operand layout, one that issues the MMAs.  While one group works on its S, the tensor cores work for the
 // other.  Waits are bounded; a CTA that gives up writes NaN.
 //
-// Measured, one B200: 2,048 queries x 32 heads (4 per KV head, d = 128, bf16) over 16,384 tokens 583 us = 884 TFLOP/s, 0.54 of cuBLAS; fp32
-// (four times the MMAs) 1,240 us; a prompt of 4,096 tokens 391 us.  A tile of 128 keys takes about 4,700 cycles, its MMAs 2,050 of them
+// Measured, one B200: 2,048 queries x 32 heads (4 per KV head, d = 128, bf16) over 16,384 tokens 558 us = 924 TFLOP/s, 0.57 of cuBLAS; fp32
+// (four times the MMAs) 1,225 us; a prompt of 4,096 tokens 366 us.  A tile of 128 keys takes about 4,700 cycles, its MMAs 2,050 of them
 // and the exponentials 2,050 (both row tiles): what binds is the chain of one row tile, scores - maximum - weights - sum - next scores,
 // of which two are in flight.  Scores of 64 keys in two buffers, asked for ahead (694 us), lengthen the MMAs instead: with N = 64 they
 // are bound by the reads of the queries from shared memory.  Fewer unrolled copies of the code gained 15 %: 16 warps in four roles fetch

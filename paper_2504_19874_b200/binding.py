@@ -383,8 +383,11 @@ def tq_kv8_attend_workspace_bytes(cache: Kv8Cache, nseq: int, n: int, q_per_kv: 
     return lib().tq_kv8_attend_workspace_bytes(cache.handle, nseq, n, q_per_kv, max_queries, nlist)
 
 
-def tq_kv8_attend(cache: Kv8Cache, table, tokens, Q, scale: float, out, workspace, lse=None, starts=None, max_queries: int = 1, lists=None):
-    """Attention of Q [n, heads * q_per_kv, d] over the sequences' caches (or, with lists [n, heads, nlist], over the listed pages)."""
+def tq_kv8_attend(cache: Kv8Cache, table, tokens, Q, scale: float, out, workspace, lse=None, starts=None, max_queries=None, lists=None):
+    """Attention of Q [n, heads * q_per_kv, d] over the sequences' caches (or, with lists [n, heads, nlist], over the listed pages).
+    max_queries: the largest number of rows of a sequence; without it, all rows may be one sequence's (one each without starts)."""
+    if max_queries is None:
+        max_queries = 1 if starts is None else Q.shape[0]
     _check((_n or _native()).kv8_attend(cache, table, tokens, starts, Q, scale, out, lse, max_queries, lists, workspace))
 
 

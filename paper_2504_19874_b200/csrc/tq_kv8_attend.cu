@@ -635,73 +635,88 @@ __global__ void __launch_bounds__(kThreads, Kernel<T, D, E4M3, NT>::kCtas) atten
 // look after several shares cost short calls 2.
 constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32, kJoinParts = 8;
 template <typename T, int D>
-__global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ AttendArgs a, int c2) {   // c2: 1, 2, 4 or 8 columns at most
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ AttendArgs a, int c2) {   // c2: 1, 2, 4 or 8 columns at a time
   __shared__ float4 o_s[kJoinWarps][32];
   wait_for_predecessor();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, first = blockIdx.x;
-  const int runs = kJoinWarps / c2, j = 8 * blockIdx.y + warp % c2, run = warp / c2;
-  const float* po = a.part_o + (int64_t)j * D + 4 * min(lane, D / 4 - 1);
+  const int runs = kJoinWarps / c2, run = warp / c2;
+  int j = 8 * blockIdx.y + warp % c2;
   auto slot = [&](int i) { return 2 * min(first + i, (int)gridDim.x - 1) + (i == 0 ? 1 : 0); };
   float4 v[kJoinParts];
   auto fetch = [&](int i0) {
+    const float* po = a.part_o + (int64_t)j * D + 4 * min(lane, D / 4 - 1);
 #pragma unroll
     for (int i = 0; i < kJoinParts; ++i) v[i] = *reinterpret_cast<const float4*>(po + (int64_t)slot(i0 + i * runs) * a.pitch * D);
   };
   const Meta z = a.meta[first];
-  const float* ml = a.part_ml + j;
-  const float m0 = ml[(int64_t)slot(lane) * 2 * a.pitch], l0 = ml[(int64_t)slot(lane) * 2 * a.pitch + a.pitch];
+  float m0, l0;
+  auto fetch_ml = [&] {
+    m0 = a.part_ml[(int64_t)slot(lane) * 2 * a.pitch + j];
+    l0 = a.part_ml[(int64_t)slot(lane) * 2 * a.pitch + a.pitch + j];
+  };
+  fetch_ml();
   fetch(run);
   const int cols = min(z.cols - 8 * (int)blockIdx.y, 8), parts = z.last_cta - first + 1;
-  if (z.last_cta < 0 || cols <= 0) return;
-  const bool mine = j - 8 * (int)blockIdx.y < cols;
-  float best = lane < parts ? m0 : -TQ_INF;
-  for (int i = lane + 32; i < parts; i += 32) best = fmaxf(best, ml[(int64_t)slot(i) * 2 * a.pitch]);
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, o));
-  float sum = 0.f;
-  float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (z.last_cta < 0) return;
 #pragma unroll 1
-  for (int p0 = 0; p0 < parts; p0 += 32) {   // weights of 32 parts, one per lane
-    float w = 0.f;
-    if (p0 + lane < parts) {
-      const int64_t at = (int64_t)slot(p0 + lane) * 2 * a.pitch;
-      w = best == -TQ_INF ? 1.f : ex2((p0 == 0 ? m0 : ml[at]) - best);
-      sum += (p0 == 0 ? l0 : ml[at + a.pitch]) * w;
+  for (int base = 0; base < cols; base += c2) {   // once, unless the caller's max_queries was too small
+    if (base > 0) {
+      j += c2;
+      fetch_ml();
+      fetch(run);
     }
-    const int end = min(p0 + 32, parts);
-#pragma unroll 1
-    for (int i0 = p0 + run; i0 < end; i0 += kJoinParts * runs) {
-      if (i0 != run) fetch(i0);
+    const float* ml = a.part_ml + j;
+    const bool mine = j - 8 * (int)blockIdx.y < cols;
+    float best = lane < parts ? m0 : -TQ_INF;
+    for (int i = lane + 32; i < parts; i += 32) best = fmaxf(best, ml[(int64_t)slot(i) * 2 * a.pitch]);
 #pragma unroll
-      for (int i = 0; i < kJoinParts; ++i) {
-        const int at = i0 + i * runs;
-        const float wi = __shfl_sync(0xffffffffu, w, (at - p0) & 31);
-        if (at < end) {                      // what is behind may not be a number
-          y.x = fmaf(v[i].x, wi, y.x); y.y = fmaf(v[i].y, wi, y.y); y.z = fmaf(v[i].z, wi, y.z); y.w = fmaf(v[i].w, wi, y.w);
+    for (int o = 16; o > 0; o >>= 1) best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, o));
+    float sum = 0.f;
+    float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+    for (int p0 = 0; p0 < parts; p0 += 32) {      // weights of 32 parts, one per lane
+      float w = 0.f;
+      if (p0 + lane < parts) {
+        const int64_t at = (int64_t)slot(p0 + lane) * 2 * a.pitch;
+        w = best == -TQ_INF ? 1.f : ex2((p0 == 0 ? m0 : ml[at]) - best);
+        sum += (p0 == 0 ? l0 : ml[at + a.pitch]) * w;
+      }
+      const int end = min(p0 + 32, parts);
+#pragma unroll 1
+      for (int i0 = p0 + run; i0 < end; i0 += kJoinParts * runs) {
+        if (i0 != run) fetch(i0);
+#pragma unroll
+        for (int i = 0; i < kJoinParts; ++i) {
+          const int at = i0 + i * runs;
+          const float wi = __shfl_sync(0xffffffffu, w, (at - p0) & 31);
+          if (at < end) {                         // what is behind may not be a number
+            y.x = fmaf(v[i].x, wi, y.x); y.y = fmaf(v[i].y, wi, y.y); y.z = fmaf(v[i].z, wi, y.z); y.w = fmaf(v[i].w, wi, y.w);
+          }
         }
       }
     }
-  }
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);   // every warp of a column has the whole sum
-  o_s[warp][lane] = y;
-  __syncthreads();
-  if (!mine || run != 0) return;
-  for (int r = 1; r < runs; ++r) {
-    const float4 x = o_s[warp + r * c2][lane];
-    y.x += x.x; y.y += x.y; y.z += x.z; y.w += x.w;
-  }
-  const int jc = z.col0 + j, g = a.g;
-  const int64_t row = (int64_t)z.row0 + jc / g;
-  const int head = z.head * g + jc % g;
-  if (lane < D / 4) {
-    T* out = static_cast<T*>(a.out) + row * a.ldo + (int64_t)head * a.ho + 4 * lane;
-    const float x[4] = {y.x, y.y, y.z, y.w};
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);   // every warp of a column has the whole sum
+    if (base > 0) __syncthreads();                // the last columns' results have been read
+    o_s[warp][lane] = y;
+    __syncthreads();
+    if (!mine || run != 0) continue;
+    for (int r = 1; r < runs; ++r) {
+      const float4 x = o_s[warp + r * c2][lane];
+      y.x += x.x; y.y += x.y; y.z += x.z; y.w += x.w;
+    }
+    const int jc = z.col0 + j, g = a.g;
+    const int64_t row = (int64_t)z.row0 + jc / g;
+    const int head = z.head * g + jc % g;
+    if (lane < D / 4) {
+      T* out = static_cast<T*>(a.out) + row * a.ldo + (int64_t)head * a.ho + 4 * lane;
+      const float x[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) store_out<T>(out + i, sum == 0.f ? 0.f : x[i] / sum);
+      for (int i = 0; i < 4; ++i) store_out<T>(out + i, sum == 0.f ? 0.f : x[i] / sum);
+    }
+    if (lane == 0 && a.lse) a.lse[row * ((int64_t)a.c.heads * g) + head] =
+        sum == 0.f ? -TQ_INF : (best == -TQ_INF ? 0.f : (best - a.lift) * kLn2) + logf(sum);
   }
-  if (lane == 0 && a.lse) a.lse[row * ((int64_t)a.c.heads * g) + head] =
-      sum == 0.f ? -TQ_INF : (best == -TQ_INF ? 0.f : (best - a.lift) * kLn2) + logf(sum);
 }
 
 template <typename T, int D, bool E4M3, int NT>
@@ -759,7 +774,7 @@ static cudaError_t join_t(const AttendArgs& a, dim3 grid, int c2, cudaStream_t s
 }
 cudaError_t launch_join(const AttendArgs& a, int dtype, int ctas, int cols, cudaStream_t st) {
   const dim3 g((unsigned)ctas, (unsigned)((cols + 7) / 8));
-  const int c2 = cols > 4 ? 8 : (cols > 2 ? 4 : cols);
+  const int c2 = cols > 4 ? 8 : (cols > 2 ? 4 : cols);   // as many as there should be
   return dtype == TQ_F32 ? join_t<float>(a, g, c2, st) : join_t<__nv_bfloat16>(a, g, c2, st);
 }
 
@@ -819,8 +834,8 @@ extern "C" int tq_kv8_attend(const tq_kv8* cache, const int32_t* table, int64_t 
   TQ_REQUIRE(workspace != nullptr && workspace_bytes >= need, TQ_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", who, workspace_bytes, need);
   TQ_REQUIRE((reinterpret_cast<uintptr_t>(workspace) & 255) == 0, TQ_ERR_ALIGNMENT, "%s: workspace is not 256-byte aligned", who);
   // units of 64 tokens, over all heads and blocks of eight columns, are numbered in 31 bits
-  const double units = (lists ? (double)n * (((double)nlist * cache->page_tokens + 63) / 64 + 1) * ((q_per_kv + 7) / 8)
-                              : ((double)nseq * 2 + (double)n * q_per_kv / 128) * (((double)width * cache->page_tokens + 63) / 64 + 1)) * cache->heads;
+  const double units = (lists != nullptr ? (double)n * (((double)nlist * cache->page_tokens + 63) / 64 + 1) * ((q_per_kv + 7) / 8)
+                              : ((double)nseq + (double)n * q_per_kv / 8) * (((double)width * cache->page_tokens + 63) / 64 + 1)) * cache->heads;
   TQ_REQUIRE(units < 2.0e9 && (double)n * q_per_kv < 2.0e9, TQ_ERR_UNSUPPORTED, "%s: %.3g units of 64 tokens in one call", who, units);
   int dev = 0, sms = 0;
   TQ_CHECK_CUDA(cudaGetDevice(&dev), who);
@@ -832,7 +847,9 @@ extern "C" int tq_kv8_attend(const tq_kv8* cache, const int32_t* table, int64_t 
   const int64_t cols = lists ? q_per_kv : (int64_t)max_queries * q_per_kv;
   const bool e4m3 = cache->code_type == TQ_E4M3, many = lists == nullptr && cols > kMaxCols;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  a.most_cols = many && nseq == 1 ? 0 : kMaxCols;   // a single sequence goes to one kernel, however many rows it turns out to have
+  // A single sequence goes to one kernel, however many rows it turns out to have, and where max_queries says that all are small, sequences
+  // that are not are still the few-query kernel's, 16 columns at a time.
+  a.most_cols = !many ? INT32_MAX : (nseq == 1 ? 0 : kMaxCols);
   if (many) {
     TQ_CHECK_CUDA(launch_prompt(a, dtype, e4m3, sms, static_cast<char*>(workspace) + attend_space(sms, a.c.d), st), who);
     count_launches(2);

@@ -167,6 +167,20 @@ def test_attend_prompts(x, dtype, d, g, page):
     check_attend(bt, bt.randn(216, 2 * g, x), 1.0 / math.sqrt(d), starts, max_queries=75)
 
 
+@pytest.mark.parametrize("most", [1, 5, 33, 1000, None])
+def test_attend_with_a_wrong_largest_number_of_rows(most):
+    """It chooses kernels; the results are the same to within their tolerances."""
+    bt = Batch([90, 20, 64], d=64, page=32, dtype=E4M3, seed=17).cuda()
+    starts = torch.tensor([0, 33, 34, 60], dtype=torch.int32)
+    Q = bt.randn(60, 6, torch.bfloat16)
+    if most is not None:
+        check_attend(bt, Q, 0.15, starts, max_queries=most)
+        return
+    q, out = Q.to(DEV), torch.zeros((60, 6, 64), dtype=torch.bfloat16, device=DEV)
+    tq.tq_kv8_attend(bt.cache, bt.t, bt.n, q, 0.15, out, workspace(tq.tq_kv8_attend_workspace_bytes(bt.cache, 3, 60, 3, 60)), starts=starts.to(DEV))
+    assert torch.equal(out, run_attend(bt, Q, 0.15, starts, max_queries=60)[0])
+
+
 @pytest.mark.parametrize("x", [torch.bfloat16, torch.float32])
 def test_attend_blocks_of_very_different_magnitudes(x):
     bt = Batch([500, 90], d=64, page=16, dtype=I8, seed=4, spread=18).cuda()

@@ -178,7 +178,9 @@ __global__ void __launch_bounds__(NT) append_kernel(const __grid_constant__ Appe
   else s1 = fmaxf(s0, block_scale<E4M3>(most));
   const float inv = block_inverse(s1), ratio = s0 * inv;
   const bool grown = p0 > 0 && s1 == s1 && s1 != s0;
-  if (bounds) {
+  // One token into blocks whose scale holds it: its lanes have a channel each to themselves, and the stored bounds suffice.
+  const bool one = NT == 32 && !grown;
+  if (bounds && !one) {
     for (int c = t; c < d; c += NT) {
       const bool keep = p0 > 0 && !grown;
       hi[c] = keep ? bounds[c] : -128;
@@ -226,13 +228,33 @@ __global__ void __launch_bounds__(NT) append_kernel(const __grid_constant__ Appe
       }
       const uint2 o = make_uint2(encode4<E4M3>(y[0], y[1], y[2], y[3]), encode4<E4M3>(y[4], y[5], y[6], y[7]));
       *reinterpret_cast<uint2*>(codes + slot * d + ch) = o;
-      if (bounds && !aligned) {
+      if (bounds && one) {
+        uint2* at = reinterpret_cast<uint2*>(bounds + ch);
+        uint2* under = reinterpret_cast<uint2*>(bounds + d + ch);
+        const uint2 h = p0 > 0 ? *at : make_uint2(0x80808080u, 0x80808080u), g = p0 > 0 ? *under : make_uint2(0x7F7F7F7Fu, 0x7F7F7F7Fu);
+        uint32_t up[2] = {o.x, o.y}, down[2] = {o.x, o.y};   // int8: a code bounds itself
+        if (E4M3) {
+#pragma unroll
+          for (int w = 0; w < 2; ++w) {
+            const uint32_t c = w ? o.y : o.x;
+            up[w] = down[w] = 0u;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const float f = decode<E4M3>((uint8_t)(c >> (8 * j))) * 0.25f;
+              up[w] |= (uint32_t)(uint8_t)__float2int_ru(f) << (8 * j);
+              down[w] |= (uint32_t)(uint8_t)__float2int_rd(f) << (8 * j);
+            }
+          }
+        }
+        *at = make_uint2(__vmaxs4(h.x, up[0]), __vmaxs4(h.y, up[1]));
+        *under = make_uint2(__vmins4(g.x, down[0]), __vmins4(g.y, down[1]));
+      } else if (bounds && !aligned) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) bound(ch + j, (uint8_t)((j < 4 ? o.x : o.y) >> (8 * (j & 3))));
       }
     }
   }
-  if (bounds && aligned) {
+  if (bounds && aligned && !one) {
     for (int x = dv; x < 32; x <<= 1)
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
@@ -248,7 +270,7 @@ __global__ void __launch_bounds__(NT) append_kernel(const __grid_constant__ Appe
     }
   }
   if (t == 0) *scale = s1;
-  if (bounds) {
+  if (bounds && !one) {
     __syncthreads();
     for (int c = t; c < d; c += NT) {
       bounds[c] = (int8_t)hi[c];

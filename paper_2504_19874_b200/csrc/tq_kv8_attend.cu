@@ -16,7 +16,7 @@
 //
 // Measured, one B200, 8 KV heads x 4 queries, d = 128: 37 sequences of 8,192 tokens stream at 5.0 TB/s, a ragged batch of 64 (563 MB) at
 // 4.9 TB/s (115 us; 0.75 of the copy bandwidth), one sequence of 32,768 tokens 27 us, of which the loop takes 10 us at the copy bandwidth
-// and the chain of first loads, the last sums and the join the rest; 1,000 tokens 9.0 us.  Reading the tiles straight into registers,
+// and the chain of first loads, the last sums and the join the rest; 1,000 tokens 9.6 us.  Reading the tiles straight into registers,
 // one step ahead, took 228 us for the batch and 43 us for the layer: eight warps per SM had too few bytes on their way.  Long calls
 // are bound by HBM; half of the issue slots and of the ALU pipe, which unpacks the codes, are in use meanwhile.
 #include <algorithm>
@@ -178,6 +178,14 @@ __global__ void __launch_bounds__(kThreads, Kernel<T, D, E4M3, NT>::kCtas) atten
   Shape sh;
   int list_units = 0;
   const int T_ = 1 << a.c.page_shift;
+  const int grid = gridDim.x;
+  // A share that ends one item and begins the next pays for its first loads and last sums twice, about as much as kCross units.  Where
+  // there are fewer items than CTAs, shares are therefore laid so that each lies within one item (items count as a multiple of `per`
+  // then, the units behind their end being empty), unless that makes them longer by more than that: nine sequences of up to five
+  // tokens 19.8 -> 18.0 us, a head's 32,768 tokens 27.7 -> 27.4, the pages of 24 rows 43.1 -> 42.4.
+  constexpr int kCross = 4;
+  int pad = 1;                          // units of an item are counted up to a multiple of this
+  auto padded = [&](int units) -> int { return pad == 1 ? units : (units + pad - 1) / pad * pad; };
   if (a.lists == nullptr) {
     int upto = 0, own = 0;
     auto units_of = [&](int b) -> int {
@@ -185,12 +193,34 @@ __global__ void __launch_bounds__(kThreads, Kernel<T, D, E4M3, NT>::kCtas) atten
       const Shape s = shape_of(a, b, NC);
       return s.units * s.blocks * a.c.heads;
     };
+    if (a.b.nseq <= kThreads) {
+      Shape s;
+      s.units = s.blocks = 0;
+      if (t < a.b.nseq) s = shape_of(a, t, NC);
+      const int items_of = s.units > 0 ? s.blocks * a.c.heads : 0;
+      own = s.units * items_of;
+      total = block_total(own, sums, &upto);
+      per = max((total + grid - 1) / grid, 1);
+      if (per > 1) {
+        int before;
+        const int items = block_total(items_of, sums, &before);
+        if (items < grid) {             // each item ends in at most one share that is not full
+          const int even = (total + grid - items - 1) / (grid - items);
+          if (even <= per + kCross) {
+            per = pad = even;
+            own = padded(s.units) * items_of;
+            total = block_total(own, sums, &upto);
+          }
+        }
+      }
+    } else {
 #pragma unroll 1
-    for (int b0 = 0; b0 < a.b.nseq; b0 += kThreads) {
-      own = units_of(b0 + t);
-      total += block_total(own, sums, &upto);
+      for (int b0 = 0; b0 < a.b.nseq; b0 += kThreads) {
+        own = units_of(b0 + t);
+        total += block_total(own, sums, &upto);
+      }
+      per = max((total + grid - 1) / grid, 1);
     }
-    per = max((total + (int)gridDim.x - 1) / (int)gridDim.x, 1);
     const int u0 = cta * per;
     if (u0 < total) {
       int before = 0;
@@ -215,6 +245,7 @@ __global__ void __launch_bounds__(kThreads, Kernel<T, D, E4M3, NT>::kCtas) atten
       seq = sums[4];
       const int from = sums[5];
       sh = shape_of(a, seq, NC);
+      sh.units = padded(sh.units);
       const int i = (u0 - from) / sh.units;
       head = i / sh.blocks;
       block = i - head * sh.blocks;
@@ -228,9 +259,16 @@ __global__ void __launch_bounds__(kThreads, Kernel<T, D, E4M3, NT>::kCtas) atten
     }
     sh.blocks = (a.g + NC - 1) / NC;
     list_units = max((int)((((int64_t)a.nlist << a.c.page_shift) + kUnit - 1) / kUnit), 1);
-    const int of_row = a.c.heads * sh.blocks;
-    total = (int)rows * of_row * list_units;
-    per = max((total + (int)gridDim.x - 1) / (int)gridDim.x, 1);
+    const int of_row = a.c.heads * sh.blocks, items = (int)rows * of_row;
+    per = max((items * list_units + grid - 1) / grid, 1);
+    if (per > 1 && items <= grid) {
+      const int shares = min(grid / items, list_units), even = (list_units + shares - 1) / shares;
+      if (even <= per + kCross) {
+        per = pad = even;
+        list_units = padded(list_units);
+      }
+    }
+    total = items * list_units;
     const int i = cta * per / list_units;
     seq = i / of_row;                                           // a row here
     head = (i - seq * of_row) / sh.blocks;
@@ -622,8 +660,10 @@ __global__ void __launch_bounds__(kThreads, Kernel<T, D, E4M3, NT>::kCtas) atten
       if (++head == a.c.heads) {
         head = 0;
         ++seq;
-        if (a.lists == nullptr)
+        if (a.lists == nullptr) {
           for (sh = shape_of(a, seq, NC); sh.units == 0; sh = shape_of(a, seq, NC)) ++seq;   // u < total: there is one
+          sh.units = padded(sh.units);
+        }
       }
     }
   }

@@ -253,6 +253,31 @@ def test_attend_many_sequences_and_long_ones():
     check_attend(bt, Q, 0.3)
 
 
+@pytest.mark.parametrize("lens,heads", [([20000, 9001, 5, 0, 3000], 2),              # few items, several units each: shares end with items
+                                        ([(i * 61) % 90 + 180 for i in range(100)], 4)])   # as many items as CTAs: shares cross them
+@pytest.mark.parametrize("x", [torch.bfloat16, torch.float32])
+def test_attend_work_laid_out_both_ways(lens, heads, x):
+    bt = Batch(lens, heads=heads, d=32, page=128, seed=len(lens)).cuda()
+    check_attend(bt, bt.randn(len(lens), 2 * heads, x), 0.2)
+
+
+def test_attend_of_steps_and_prompts_in_one_batch_of_many():
+    """600 sequences, most of them with one row: those go to one kernel, the few with 21 to the other."""
+    lens = [(i * 13) % 60 + 30 for i in range(600)]
+    bt = Batch(lens, heads=1, d=32, page=16, dtype=E4M3, seed=31).cuda()
+    rows = [21 if i % 50 == 7 else (0 if i % 90 == 5 else 1) for i in range(600)]
+    starts = torch.tensor([0] + rows).cumsum(0).to(torch.int32)
+    check_attend(bt, bt.randn(int(starts[-1]) + 1, 1, torch.bfloat16), 0.2, starts, max_queries=21)
+
+
+def test_attend_long_lists():
+    bt = Batch([30000, 17000, 100], heads=2, d=32, page=128, seed=5).cuda()
+    starts = torch.tensor([0, 3, 5, 6], dtype=torch.int32)
+    Q = bt.randn(6, 4, torch.bfloat16)
+    lists = ref.select(bt.pool, bt.table, bt.tokens, Q, 70, starts=starts)
+    check_attend(bt, Q, 0.2, starts, max_queries=3, lists=lists)
+
+
 # ---------------------------------------------------------------------------------------------------------------- select and lists
 
 @pytest.mark.parametrize("x", [torch.bfloat16, torch.float32])

@@ -187,6 +187,14 @@ def test_attend_blocks_of_very_different_magnitudes(x):
     check_attend(bt, bt.randn(2, 4, x) * 2.0 ** -12, 1.0)
 
 
+@pytest.mark.parametrize("x", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("scale", [-0.2, 0.0])
+def test_attend_with_a_negative_scale_and_without_one(scale, x):
+    bt = Batch([150, 40], d=64, page=32, dtype=I8, seed=23).cuda()
+    check_attend(bt, bt.randn(2, 4, x), scale)
+    check_attend(bt, bt.randn(45, 4, x), scale, torch.tensor([0, 40, 45], dtype=torch.int32), max_queries=40)
+
+
 def test_attend_passes_over_pages_that_are_none():
     bt = Batch([100, 50], d=64, page=16, dtype=E4M3, seed=9).cuda()
     bt.table[0, 2], bt.table[0, 6], bt.table[1, :] = -1, 1 << 30, -5

@@ -2,13 +2,16 @@
 //
 // Mathematics.  Columns are the queries that share a KV head (q_per_kv heads of up to a few tokens, 8 or 16 at a time); per 16 tokens
 //   S^T = K Q^T   (16 tokens x 8 columns, one mma per 16 channels: the codes are the A operand, converted to fp16 exactly),
-//   p = 2^(s - m + 6) with the column's running maximum m,   O^T += V^T P^T   (P^T is S^T transposed in registers).
-// m only moves when a score exceeds it by 2^8, so most steps rescale nothing; p <= 2^14 stays inside fp16.
+//   l += 2^(s - m + 6) with the column's running maximum m,   p = 2^(s + log2 v - r + 6),   O^T += V^T P^T
+// (P^T is S^T transposed in registers), v the scale of the tile's values and r the column's running maximum of s + log2 v: what goes into
+// the matrix product is a weight times a scale, relative to the largest such product so far, so neither a page of far larger or
+// smaller values nor its order can push the others' bits out of fp16 or the sums out of fp32.  out = O 2^(r - m) / l.
+// m and r are whole numbers and only rise, when a score exceeds one of them by 2^8, so most steps rescale nothing and those that do
+// multiply by exact powers of two up to 1; p <= 2^14 stays inside fp16.
 // Queries are scaled per row by a power of two into [2^13, 2^14): bf16 values are then exact in fp16 (an element 2^-30 of the row's
 // largest loses bits), and fp32 values are two fp16 limbs (2^-23 of each value).  P is one fp16 limb for bf16 outputs (2^-12 of each
 // weight, an eighth of the output's own rounding) and two for fp32 ones.  All sums are fp32.
-// Scales are powers of two: the key's goes into the score's factor, the value's into p, relative to a unit u of the accumulator that
-// follows the largest scale (exact; P keeps its bits while scales stay within 2^4 of u, and u moves where they do not).
+// Scales are powers of two: the key's goes into the score's factor, the value's into p's exponent, both exactly.
 //
 // Work.  Units of 64 tokens of one (sequence, head) are numbered through; every CTA takes an equal share of them, whatever the lengths,
 // and of a unit each of its four warps takes 16 tokens, through a ring of its own in shared memory, some steps ahead.  Warps are
@@ -40,6 +43,12 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
   uint32_t y;
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
+}
+// log2 of a block's scale: exact for a power of two, -inf for 0 and for NaN (whose weights are set apart).
+__device__ __forceinline__ float scale_log2(float s) {
+  const uint32_t u = __float_as_uint(s);
+  if ((u & 0x7FFFFFu) == 0u && u - 1u < 0x7F7FFFFFu) return (float)((int)(u >> 23) - 127);
+  return s > 0.f ? __log2f(s) : -TQ_INF;
 }
 __device__ __forceinline__ uint32_t half2_bits(float lo, float hi) {
   const __half2 h = __floats2half2_rn(lo, hi);
@@ -319,11 +328,10 @@ __global__ void __launch_bounds__(kThreads, Kernel<T, D, E4M3, NT>::kCtas) atten
       vis_min = (int)max(tokens - (len_q - 1 - col0 / width_c), (int64_t)0);
       vis_max = (int)max(tokens - (len_q - 1 - (col0 + cols - 1) / width_c), (int64_t)0);
     }
-    float m[NT][2], l[NT][2], o[2 * VW][NT][4];
-    float unit = 0.f, last_vs = 0.f, ratio = 0.f;
+    float m[NT][2], mv[NT][2], l[NT][2], o[2 * VW][NT][4];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      m[nt][0] = m[nt][1] = -TQ_INF;
+      m[nt][0] = m[nt][1] = mv[nt][0] = mv[nt][1] = -TQ_INF;
       l[nt][0] = l[nt][1] = 0.f;
 #pragma unroll
       for (int j = 0; j < 2 * VW; ++j) o[j][nt][0] = o[j][nt][1] = o[j][nt][2] = o[j][nt][3] = 0.f;
@@ -458,6 +466,7 @@ __global__ void __launch_bounds__(kThreads, Kernel<T, D, E4M3, NT>::kCtas) atten
           }
       }
       const bool edge = t0 + 16 > vis_min;      // some column does not see all 16 tokens
+      const float lv = scale_log2(vs);
       bool higher = false;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
@@ -468,7 +477,9 @@ __global__ void __launch_bounds__(kThreads, Kernel<T, D, E4M3, NT>::kCtas) atten
           for (int e = 0; e < 4; ++e)
             if (t0 + n8 + 8 * (e >> 1) >= vis[nt][e & 1]) s[nt][e] = -TQ_INF;
         }
-        higher |= fmaxf(s[nt][0], s[nt][2]) > m[nt][0] + kSlack || fmaxf(s[nt][1], s[nt][3]) > m[nt][1] + kSlack;
+#pragma unroll
+        for (int e = 0; e < 2; ++e)     // (values of no scale, mv - lv = NaN or +inf: m alone)
+          higher |= fmaxf(s[nt][e], s[nt][2 + e]) > fminf(m[nt][e], mv[nt][e] - lv) + kSlack;
       }
       if (__any_sync(0xffffffffu, higher)) {
 #pragma unroll
@@ -479,10 +490,11 @@ __global__ void __launch_bounds__(kThreads, Kernel<T, D, E4M3, NT>::kCtas) atten
             g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, 4));
             g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, 8));
             g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, 16));
-            const float top_m = fmaxf(m[nt][e], g);
-            const float alpha = top_m > m[nt][e] ? ex2(m[nt][e] - top_m) : 1.f;    // m = -inf: 0
+            const float top_m = fmaxf(m[nt][e], ceilf(g)), top_v = fmaxf(mv[nt][e], ceilf(g + lv));
+            l[nt][e] *= top_m > m[nt][e] ? ex2(m[nt][e] - top_m) : 1.f;                 // from -inf: 0
+            const float alpha = top_v > mv[nt][e] ? ex2(mv[nt][e] - top_v) : 1.f;
             m[nt][e] = top_m;
-            l[nt][e] *= alpha;
+            mv[nt][e] = top_v;
 #pragma unroll
             for (int j = 0; j < 2 * VW; ++j) {
               o[j][nt][e] *= alpha;
@@ -490,39 +502,17 @@ __global__ void __launch_bounds__(kThreads, Kernel<T, D, E4M3, NT>::kCtas) atten
             }
           }
       }
-      if (vs != last_vs) {                        // the unit of the accumulators follows the largest scale
-        last_vs = vs;
-        if (!(vs == vs)) {
-          ratio = vs;
-          last_vs = 0.f;                            // NaN: looked at again for the next tile
-        } else if (vs == 0.f) {
-          ratio = 0.f;
-        } else if (unit == 0.f || vs > unit || (vs < unit * 0.0625f && unit < vs * 1e18f)) {
-          const float back = unit / vs;
-#pragma unroll
-          for (int j = 0; j < 2 * VW; ++j)
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) o[j][nt][e] *= back;
-          unit = vs;
-          ratio = 1.f;
-        } else {
-          ratio = vs / unit;
-        }
-      } else if (vs == 0.f) {
-        ratio = 0.f;
-      }
       uint32_t p[NT][LIMBS][2];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         float y[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float mm = m[nt][e & 1];
-          y[e] = ex2(s[nt][e] + (mm == -TQ_INF ? 0.f : kLift - mm));
-          l[nt][e & 1] += y[e];
-          y[e] = edge && y[e] == 0.f ? 0.f : y[e] * ratio;    // what a column does not see adds nothing, NaN or not
+          const float mm = m[nt][e & 1], mw = mv[nt][e & 1];
+          const float x = ex2(s[nt][e] + (mm == -TQ_INF ? 0.f : kLift - mm));
+          l[nt][e & 1] += x;
+          y[e] = ex2(s[nt][e] + (mw == -TQ_INF ? -TQ_INF : kLift + (lv - mw)));
+          if (!(vs == vs)) y[e] = edge && x == 0.f ? 0.f : vs;   // what a column does not see adds nothing, NaN or not
         }
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
@@ -611,11 +601,13 @@ __global__ void __launch_bounds__(kThreads, Kernel<T, D, E4M3, NT>::kCtas) atten
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const int j = nt * 8 + 2 * c4 + e;
-        const float w = (top[j] == -TQ_INF ? 1.f : ex2(m[nt][e] - top[j])) * unit;
+        // divided by the whole sum here: an average of the values, in range whatever their scales (in two steps, as 2^x may not be)
+        const float x = mv[nt][e] == -TQ_INF ? 0.f : mv[nt][e] - top[j], x0 = floorf(0.5f * x);   // nothing: O is 0, or NaN
+        const float w = ex2(x0), w1 = tot[j] == 0.f ? 0.f : ex2(x - x0) / tot[j];
 #pragma unroll
         for (int i = 0; i < 2 * VW; ++i) {
-          osm[(warp * NC + j) * K::OP + 4 * VW * n8 + 2 * i] = o[i][nt][e] * w;
-          osm[(warp * NC + j) * K::OP + 4 * VW * n8 + 2 * i + 1] = o[i][nt][2 + e] * w;
+          osm[(warp * NC + j) * K::OP + 4 * VW * n8 + 2 * i] = o[i][nt][e] * w * w1;
+          osm[(warp * NC + j) * K::OP + 4 * VW * n8 + 2 * i + 1] = o[i][nt][2 + e] * w * w1;
         }
       }
     __syncthreads();
@@ -629,7 +621,7 @@ __global__ void __launch_bounds__(kThreads, Kernel<T, D, E4M3, NT>::kCtas) atten
       if (whole) {
         const int jc = col0 + j;
         T* out = static_cast<T*>(a.out) + (row0 + jc / width_c) * a.ldo + (int64_t)(head * a.g + jc % width_c) * a.ho;
-        store_out<T>(out + ch, tot[j] == 0.f ? 0.f : y / tot[j]);
+        store_out<T>(out + ch, y);
       } else {
         a.part_o[((int64_t)slot * kMaxCols + j) * D + ch] = y;
       }
@@ -689,10 +681,13 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
     for (int i = 0; i < kJoinParts; ++i) v[i] = *reinterpret_cast<const float4*>(po + (int64_t)slot(i0 + i * runs) * a.pitch * D);
   };
   const Meta z = a.meta[first];
-  float m0, l0;
+  float mi[2], li[2];                      // of parts lane and lane + 32
   auto fetch_ml = [&] {
-    m0 = a.part_ml[(int64_t)slot(lane) * 2 * a.pitch + j];
-    l0 = a.part_ml[(int64_t)slot(lane) * 2 * a.pitch + a.pitch + j];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      mi[i] = a.part_ml[(int64_t)slot(lane + 32 * i) * 2 * a.pitch + j];
+      li[i] = a.part_ml[(int64_t)slot(lane + 32 * i) * 2 * a.pitch + a.pitch + j];
+    }
   };
   fetch_ml();
   fetch(run);
@@ -707,20 +702,21 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
     }
     const float* ml = a.part_ml + j;
     const bool mine = j - 8 * (int)blockIdx.y < cols;
-    float best = lane < parts ? m0 : -TQ_INF;
-    for (int i = lane + 32; i < parts; i += 32) best = fmaxf(best, ml[(int64_t)slot(i) * 2 * a.pitch]);
+    auto max_of = [&](int i) { return i < 32 ? mi[0] : (i < 64 ? mi[1] : ml[(int64_t)slot(i) * 2 * a.pitch]); };
+    auto sum_of = [&](int i) { return i < 32 ? li[0] : (i < 64 ? li[1] : ml[(int64_t)slot(i) * 2 * a.pitch + a.pitch]); };
+    float best = -TQ_INF;
+    for (int i = lane; i < parts; i += 32) best = fmaxf(best, max_of(i));
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, o));
+    auto weight = [&](int i) { return sum_of(i) * (best == -TQ_INF ? 1.f : ex2(max_of(i) - best)); };
     float sum = 0.f;
-    float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i = lane; i < parts; i += 32) sum += weight(i);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);   // every warp of a column has the whole sum
+    float4 y = make_float4(0.f, 0.f, 0.f, 0.f);   // parts are averages of values: with weights that add up to 1 nothing leaves their range
 #pragma unroll 1
     for (int p0 = 0; p0 < parts; p0 += 32) {      // weights of 32 parts, one per lane
-      float w = 0.f;
-      if (p0 + lane < parts) {
-        const int64_t at = (int64_t)slot(p0 + lane) * 2 * a.pitch;
-        w = best == -TQ_INF ? 1.f : ex2((p0 == 0 ? m0 : ml[at]) - best);
-        sum += (p0 == 0 ? l0 : ml[at + a.pitch]) * w;
-      }
+      const float w = p0 + lane < parts && sum != 0.f ? weight(p0 + lane) / sum : 0.f;
       const int end = min(p0 + 32, parts);
 #pragma unroll 1
       for (int i0 = p0 + run; i0 < end; i0 += kJoinParts * runs) {
@@ -735,8 +731,6 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
         }
       }
     }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);   // every warp of a column has the whole sum
     if (base > 0) __syncthreads();                // the last columns' results have been read
     o_s[warp][lane] = y;
     __syncthreads();
@@ -752,7 +746,7 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
       T* out = static_cast<T*>(a.out) + row * a.ldo + (int64_t)head * a.ho + 4 * lane;
       const float x[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
-      for (int i = 0; i < 4; ++i) store_out<T>(out + i, sum == 0.f ? 0.f : x[i] / sum);
+      for (int i = 0; i < 4; ++i) store_out<T>(out + i, x[i]);
     }
     if (lane == 0 && a.lse) a.lse[row * ((int64_t)a.c.heads * g) + head] =
         sum == 0.f ? -TQ_INF : (best == -TQ_INF ? 0.f : (best - a.lift) * kLn2) + logf(sum);

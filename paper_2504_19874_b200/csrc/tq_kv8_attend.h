@@ -30,7 +30,7 @@ struct AttendArgs {
   int64_t ldo, ho;
   float* lse;
   Meta* meta;             // workspace
-  float *part_ml, *part_o;
+  float *part_ml, *part_o;   // parts of items: maxima and sums, and outputs divided by these sums
   int pitch;              // columns of a part
   float lift;             // of its weights
 };

@@ -589,7 +589,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
         tc::tc_fence_after();
         const bool whole = u == item_at && u + n == item_at + it.tiles;
         const int slot = 2 * (int)blockIdx.x + (u == item_at ? 1 : 0);
-        const float by = !good ? __uint_as_float(0x7FC00000u) : (whole ? (l == 0.f ? 0.f : uv / l) : uv);
+        const float by = !good ? __uint_as_float(0x7FC00000u) : (l == 0.f ? 0.f : uv / l);   // parts are averages too
         T* out = static_cast<T*>(a.out) + q_row * a.ldo + (int64_t)q_head * a.ho;
         const bool vec_out = (reinterpret_cast<uintptr_t>(out) & 31) == 0;
         float* part = a.part_o + ((int64_t)slot * a.pitch + row) * D;
@@ -599,11 +599,11 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
           tc::tmem_ld32(o_col + 32 * j, v);
           tc::tmem_ld_wait();
           if (mine) {
-            if (whole) {
-              if (l == 0.f && good) {
+            if (l == 0.f && good) {
 #pragma unroll
-                for (int e = 0; e < 32; ++e) v[e] = 0u;
-              }
+              for (int e = 0; e < 32; ++e) v[e] = 0u;
+            }
+            if (whole) {
               store32<T>(out + 32 * j, vec_out, v, by);
             } else {
               store32<float>(part + 32 * j, true, v, by);

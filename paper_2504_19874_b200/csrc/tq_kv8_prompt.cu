@@ -1,12 +1,13 @@
 // Attention over a paged 8-bit KV cache for many queries per sequence (prompts, chunks of prompts), on tcgen05.
 //
 // Mathematics.  Rows are (token, head of the group) pairs of one sequence and KV head; per tile of 128 rows and 128 keys
-//   S = Q K^T (TMEM),  p = 2^(s - m + lift) with the row's running maximum m,  O += P V (TMEM, P as the A operand from TMEM).
-// As in the few-query kernel queries are scaled per row by a power of two into [2^13, 2^14) and held in fp16 (fp32 ones as two limbs),
-// P is one fp16 limb for bf16 outputs and two for fp32 ones, and m moves only when a score exceeds it by far: then the row's O in
-// TMEM is rescaled by its own thread.  All sums are fp32.
-// The codes become fp16 in shared memory, times their block's scale over the largest scale of the pages in hand (a power of two, so
-// exact down to 2^-24 of that scale, 2^-31 of the largest number): the one factor left per row goes into the softmax or the output.
+//   S = Q K^T (TMEM),  p = 2^(s + log2 v - r + lift),  l += 2^(r - log2 v - m) sum p,  O += P V (TMEM, P as the A operand from TMEM),
+// out = O 2^(r - m) / l.  As in the few-query kernel queries are scaled per row by a power of two into [2^13, 2^14) and held in fp16 (fp32 ones
+// as two limbs), P is one fp16 limb for bf16 outputs and two for fp32 ones, m is the row's running maximum and r that of s + log2 v, whole
+// numbers that only rise, when a score exceeds one of them by far: then the row's O in TMEM is rescaled by its own thread.  Sums are fp32.
+// v and its like for keys are the tile's units, the largest scales of its blocks.  The codes become fp16 in shared memory times their
+// block's scale over the unit, a power of two from 2^-15 to 1 and so exactly.  Blocks below that are left out (masked, as keys that nobody sees)
+// and take their turn with units of their own in a second pass over the same tile: what one page holds changes nothing for another.
 //
 // Work.  A CTA per SM; units are (tile of 128 keys) x (block of 256 rows, fp32: 128), numbered through over blocks, heads and sequences,
 // and every CTA takes an equal run of them, so that causal triangles and ragged batches are even; runs that end inside a block leave
@@ -131,8 +132,8 @@ struct Item {
 };
 struct Shared {
   Bars bar;
-  float uk[4], uv[4];                       // largest scales of the items in hand, by the item's number
-  int flags[4];                             // of tiles, by number: bits 0-7: 16 keys whose values are NaN; 8-15: 16 keys of no page
+  float2 units[4];                          // of passes, by number: scale of the keys, log2 of the values'
+  int flags[4];                             // bits 0-7: 16 keys whose values are NaN; 8-15: of no page, or of another pass; 16: the tile has another pass
   uint32_t tmem;
   int abort_flag;
   int sums[16], found[4];
@@ -480,19 +481,18 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
         }
         tc::fence_proxy_async();
         tc::mbar_arrive(&sh.bar.q_ready);
-        float m = -TQ_INF, l = 0.f, uv = 0.f;
-        for (int i = 0; i < n && ok; ++i) {
-          const int nt = n_tile + i;
+        float m = -TQ_INF, mv = -TQ_INF, l = 0.f;
+        bool fresh = true;                  // O holds nothing yet
+        for (int i = 0; i < n;) {
+          const int nt = n_tile++;
           ok = wait_all(&sh.bar.s_ready[tile], nt & 1);
           if (!ok) break;
           tc::tc_fence_after();
-          if (i == 0) {                     // written before the item's first keys, which these scores have read
-            f *= sh.uk[n_item & 3];
-            if (f < 1e-30f) f = 1e-30f;     // keys of zeros, or no scale: all scores are (nearly) 0, and -inf stays what it is
-            uv = sh.uv[n_item & 3];
-          }
-          const int t0 = (first + i) * kKeys, flags = sh.flags[nt & 3];   // bits 0-7: NaN values, 8-15: no page
-          const bool edge = t0 + kKeys > it.vis_min || flags != 0;
+          const int t0 = (first + i) * kKeys, flags = sh.flags[nt & 3];
+          const float2 unit = sh.units[nt & 3];
+          const bool edge = t0 + kKeys > it.vis_min || (flags & 0xFFFF) != 0;
+          float factor = f * unit.x;
+          if (factor < 1e-30f) factor = 1e-30f;   // keys of zeros: all scores are (nearly) 0, and -inf stays what it is
           uint32_t v[2][32];
           auto load_half = [&](int half) {
             tc::tmem_ld32(s_col + 64 * half, v[0]);
@@ -526,16 +526,19 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
             load_half(half);
             top = fmaxf(top, largest());
           }
-          top *= f;
-          const bool higher = top > m + Range<T>::kSlack;
+          top *= factor;
+          const float top_v = top + unit.y;
+          const bool higher = top > m + Range<T>::kSlack || top_v > mv + Range<T>::kSlack;
           if (__any_sync(0xffffffffu, higher)) {
             float alpha = 1.f;
             if (higher) {
-              alpha = ex2(m - top);         // 0 for the first
-              m = top;
-              l *= alpha;
+              const float new_m = fmaxf(m, ceilf(top)), new_v = fmaxf(mv, ceilf(top_v));
+              if (new_m > m) l *= ex2(m - new_m);                                 // from -inf: 0
+              if (new_v > mv) alpha = ex2(mv - new_v);
+              m = new_m;
+              mv = new_v;
             }
-            if (i > 0) {                    // O holds nothing before the first tile; it is at rest: these scores were asked for after its last sum
+            if (!fresh) {                   // O is at rest: these scores were asked for after its last sum
 #pragma unroll 1
               for (int j = 0; j < D / 16; ++j) {
                 uint32_t w[16];
@@ -547,8 +550,9 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
               }
             }
           }
-          const float shift = m == -TQ_INF ? 0.f : Range<T>::kLift - m;
-          const uint64_t f2 = both(f), shift2 = both(shift);
+          // p relative to r, but for what lies 2^60 below it: that rounds to 0 in P, and must not in l
+          const float below = fmaxf(m - mv + unit.y, -60.f), shift = m == -TQ_INF ? 0.f : Range<T>::kLift - m + below;
+          const uint64_t f2 = both(factor), shift2 = both(shift);
           uint64_t sum[2] = {0ull, 0ull};
           constexpr int W = LIMBS == 2 ? 16 : 32;   // keys per store: registers are scarce
           auto weights = [&](auto is_edge, int half) {
@@ -582,14 +586,18 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
             load_half(half);
             if (edge) weights(std::true_type{}, half); else weights(std::false_type{}, half);
           }
-          l += sum_of(sum[0]) + sum_of(sum[1]);
+          l += (sum_of(sum[0]) + sum_of(sum[1])) * ex2(-below);
+          fresh = false;
+          i += 1 - (flags >> 16);
         }
         if (ok) ok = wait_all(&sh.bar.o_done, n_item & 1);
         const bool good = ok;
         tc::tc_fence_after();
         const bool whole = u == item_at && u + n == item_at + it.tiles;
         const int slot = 2 * (int)blockIdx.x + (u == item_at ? 1 : 0);
-        const float by = !good ? __uint_as_float(0x7FC00000u) : (l == 0.f ? 0.f : uv / l);   // parts are averages too
+        // an average of the values (parts are averages too); in two steps, as the power may be out of range
+        const float x = mv == -TQ_INF ? 0.f : mv - m, x0 = floorf(0.5f * x), by0 = ex2(x0);
+        const float by = !good ? __uint_as_float(0x7FC00000u) : (l == 0.f ? 0.f : ex2(x - x0) / l);
         T* out = static_cast<T*>(a.out) + q_row * a.ldo + (int64_t)q_head * a.ho;
         const bool vec_out = (reinterpret_cast<uintptr_t>(out) & 31) == 0;
         float* part = a.part_o + ((int64_t)slot * a.pitch + row) * D;
@@ -599,10 +607,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
           tc::tmem_ld32(o_col + 32 * j, v);
           tc::tmem_ld_wait();
           if (mine) {
-            if (l == 0.f && good) {
 #pragma unroll
-              for (int e = 0; e < 32; ++e) v[e] = 0u;
-            }
+            for (int e = 0; e < 32; ++e) v[e] = l == 0.f && good ? 0u : __float_as_uint(__uint_as_float(v[e]) * by0);
             if (whole) {
               store32<T>(out + 32 * j, vec_out, v, by);
             } else {
@@ -627,7 +633,6 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
           meta->last_cta = (item_at + it.tiles - 1) / per;
         }
         tc::tc_fence_before();
-        n_tile += n;
         ++n_item;
         u += n;
         item_at += it.tiles;
@@ -646,31 +651,6 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
       while (u < u_end && ok) {
         const int n = min(u_end, item_at + it.tiles) - u, first = u - item_at;
         const int32_t* row_pages = a.b.table + (int64_t)it.b * a.b.ldt;
-        // largest scales of the pages in hand
-        float top_k = 0.f, top_v = 0.f;
-        {
-          const int64_t t_first = (int64_t)first * kKeys, t_last = min((int64_t)(first + n) * kKeys, (int64_t)it.vis_max);
-          if (t_last > t_first)
-#pragma unroll 4
-            for (int64_t j = (t_first >> a.c.page_shift) + lane; j <= (t_last - 1) >> a.c.page_shift; j += 32) {
-              const int id = row_pages[j];
-              const bool is = id >= 0 && id < a.c.pages;
-              const int64_t at = (int64_t)(is ? id : 0) * a.c.heads + it.head;
-              const float x = a.c.k_scale[at], y = a.c.v_scale[at];
-              top_k = is ? fmaxf(top_k, x) : top_k;   // NaN is passed over
-              top_v = is ? fmaxf(top_v, y) : top_v;
-            }
-#pragma unroll
-          for (int o = 16; o > 0; o >>= 1) {
-            top_k = fmaxf(top_k, __shfl_xor_sync(0xffffffffu, top_k, o));
-            top_v = fmaxf(top_v, __shfl_xor_sync(0xffffffffu, top_v, o));
-          }
-        }
-        if (!isv && we == 0 && lane == 0) {
-          sh.uk[n_item & 3] = top_k;
-          sh.uv[n_item & 3] = top_v;
-        }
-        const float inv = block_inverse(isv ? top_v : top_k);
         uint4 raw[G][N];
         // what lane l < 8 knows of keys 16 l .. 16 l + 15 of a tile: page and scales; looked up two tiles ahead
         struct Known { int id; float ks, vs; };
@@ -737,23 +717,37 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
         };
         Known now = look_up(first), next = look_up(first + 1);
         read(now.id, first, raw);
-        for (int i = 0; i < n && ok; ++i) {
-          const int nt = n_tile + i, st = nt & 1;
-          float r = now.id >= 0 ? (isv ? now.vs : now.ks) * inv : 0.f;
-          // slots of no page (those behind the last token are masked anyway), and NaN values, which become zeros: see the softmax
-          const uint32_t absent = __ballot_sync(0xffffffffu, lane < 8 && now.id < 0), nan = __ballot_sync(0xffffffffu, lane < 8 && !(now.vs == now.vs));
-          if (isv && !(r == r)) r = 0.f;
-          now = next;
-          next = look_up(first + i + 2);
+        bool left = true;                   // these keys have not been in a pass
+        for (int i = 0; i < n;) {
+          // units of what is left: scales are positive, so their bits are in their order; 0 and NaN go with any unit
+          const float uk = __uint_as_float(__reduce_max_sync(0xffffffffu, left && now.ks > 0.f ? __float_as_uint(now.ks) : 0u));
+          bool in = left && !(now.ks < uk * 0x1p-15f && now.ks > 0.f);
+          const float uv = __uint_as_float(__reduce_max_sync(0xffffffffu, in && now.vs > 0.f ? __float_as_uint(now.vs) : 0u));
+          in = in && !(now.vs < uv * 0x1p-15f && now.vs > 0.f);
+          const bool again = __any_sync(0xffffffffu, left && !in);
+          left = left && !in;
+          in = in && now.id >= 0;
+          const float x = isv ? now.vs : now.ks, r = !in || (isv && !(x == x)) ? 0.f : x * block_inverse(isv ? uv : uk);
+          const int nt = n_tile++, st = nt & 1;
+          const int flags = (int)((again ? 1u << 16 : 0u) | (__ballot_sync(0xffffffffu, !in) & 0xFFu) << 8 |
+                                  (__ballot_sync(0xffffffffu, in && !(now.vs == now.vs)) & 0xFFu));
           ok = wait_all(&empty[st], ((nt >> 1) & 1) ^ 1);
           if (!ok) break;
-          if (!isv && we == 0 && lane == 0) sh.flags[nt & 3] = (int)(((absent & 0xFFu) << 8) | (nan & 0xFFu));
+          if (!isv && we == 0 && lane == 0) {
+            sh.flags[nt & 3] = flags;
+            sh.units[nt & 3] = make_float2(uk, uv > 0.f ? scale_log2(uv) : -126.f);
+          }
           write(operand + st * OP, raw, r);
           tc::fence_proxy_async();
           tc::mbar_arrive(&full[st]);
-          read(now.id, first + i + 1, raw);
+          if (!again) {                     // else the same codes once more
+            left = true;
+            now = next;
+            ++i;
+            next = look_up(first + i + 1);
+          }
+          read(now.id, first + i, raw);
         }
-        n_tile += n;
         ++n_item;
         u += n;
         item_at += it.tiles;
@@ -793,8 +787,10 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
 #pragma unroll
         for (int tile = 0; tile < TILES; ++tile) scores(tile, n_tile & 1);
         tc::umma_commit(&sh.bar.k_empty[n_tile & 1]);
-        for (int i = 0; i < n && ok; ++i) {
-          const int nt = n_tile + i, st = nt & 1;
+        bool fresh = true;
+        for (int i = 0; i < n && ok;) {
+          const int nt = n_tile++, st = nt & 1;
+          i += 1 - (sh.flags[nt & 3] >> 16);     // the pass's keys are there, so its flags are
 #pragma unroll
           for (int part = 0; part < 2 * TILES; ++part) {   // the groups are half a tile apart: 0 first half, 0 second, 1 first, 1 second
             const int tile = part >> 1, half = part & 1;
@@ -802,8 +798,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
             if (part == 0) ok = ok && tc::mbar_wait(&sh.bar.v_full[st], (nt >> 1) & 1, abort_flag, status);
             if (!ok) break;
             tc::tc_fence_after();
-            sums(tile, half, st, i == 0 && half == 0);
-            if (half == 1 && i + 1 < n) {
+            sums(tile, half, st, fresh && half == 0);
+            if (half == 1 && i < n) {
               if (tile == 0) ok = tc::mbar_wait(&sh.bar.k_full[(nt + 1) & 1], ((nt + 1) >> 1) & 1, abort_flag, status);
               if (!ok) break;
               tc::tc_fence_after();
@@ -811,11 +807,11 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
             }
           }
           if (!ok) break;
+          fresh = false;
           tc::umma_commit(&sh.bar.v_empty[st]);
-          if (i + 1 < n) tc::umma_commit(&sh.bar.k_empty[(nt + 1) & 1]);
+          if (i < n) tc::umma_commit(&sh.bar.k_empty[(nt + 1) & 1]);
         }
         if (ok) tc::umma_commit(&sh.bar.o_done);
-        n_tile += n;
         ++n_item;
         u += n;
         item_at += it.tiles;

@@ -113,3 +113,65 @@ def test_the_largest_values(x):
     bt = Batch([100, 2000], heads=1, d=32, page=32, seed=3)
     bt.pool["v_scale"][bt.table[bt.table >= 0].long()] = 2.0 ** 120
     check(bt.cuda(), bt.randn(2, 2, x), 0.2)
+
+
+# ---------------------------------------------------------------------------------------------------------------- many queries
+
+@pytest.mark.parametrize("x", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("dtype", [I8, E4M3])
+@pytest.mark.parametrize("order", ORDERS)
+def test_values_of_prompts(order, dtype, x):
+    """Through the kernel of many queries, and through that of few (max_queries only chooses)."""
+    starts = torch.tensor([0, 45, 90], dtype=torch.int32)
+    for lens, page in (([400, 130], 16), ([700, 45], 128)):
+        bt = Batch(lens, heads=1, d=32, page=page, dtype=dtype, seed=page + 1)
+        scale_pages(bt, "v_scale", ORDERS[order])
+        bt.cuda()
+        Q = bt.randn(90, 1, x)
+        for most in (45, 1):
+            check(bt, Q, 0.2, starts, max_queries=most)
+
+
+@pytest.mark.parametrize("x", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("dtype", [I8, E4M3])
+@pytest.mark.parametrize("large", [30, 60, 100])
+@pytest.mark.parametrize("d", [32, 96, 128])
+def test_rows_before_a_late_large_page_do_not_feel_it(d, large, dtype, x):
+    """Finite values 2^large above the others in the last page of a chunk; the rows before it do not see that page."""
+    bt = Batch([330], heads=1, d=d, page=32, dtype=dtype, seed=large)
+    bt.pool["v_scale"][bt.table[0, 10]] *= 2.0 ** large
+    bt.pool["k"][bt.table[0, 10], :, :, :16] = torch.full((), 96.0).to(dtype)       # keys too, in channels that queries leave at 0
+    bt.pool["k"][bt.table[0, 10], :, :, 16:] = torch.zeros((), dtype=torch.int8).view(dtype) if dtype == I8 else torch.zeros(()).to(dtype)
+    bt.pool["k_scale"][bt.table[0, 10]] *= 2.0 ** large
+    Q = bt.randn(120, 2, x)
+    Q[..., :16] = 0.0
+    check(bt.cuda(), Q, 0.3, torch.tensor([0, 120], dtype=torch.int32), max_queries=120)
+
+
+@pytest.mark.parametrize("x", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("dtype", [I8, E4M3])
+@pytest.mark.parametrize("spread", [18, 30, 50])
+def test_keys_of_prompts(spread, dtype, x):
+    """Keys of many magnitudes: the large ones in channels that queries leave at 0."""
+    bt = Batch([500, 90], heads=2, d=64, page=16, dtype=dtype, seed=spread)
+    for row in bt.table.tolist():
+        for j, p in enumerate(row):
+            if p >= 0 and j % 3 == 1:
+                bt.pool["k"][p, :, :, 16:] = torch.zeros(()).to(dtype)
+                bt.pool["k_scale"][p] *= 2.0 ** spread
+            elif p >= 0 and j % 3 == 2:
+                bt.pool["k_scale"][p] *= 2.0 ** -spread
+    bt.cuda()
+    Q = bt.randn(60, 4, x)
+    Q[..., :16] = 0.0
+    for most in (40, 1):
+        check(bt, Q, 0.2, torch.tensor([0, 40, 60], dtype=torch.int32), max_queries=most)
+
+
+@pytest.mark.parametrize("x", [torch.bfloat16, torch.float32])
+def test_the_largest_and_no_values_of_prompts(x):
+    bt = Batch([100, 300], heads=1, d=32, page=32, seed=3)
+    bt.pool["v_scale"][bt.table[bt.table >= 0].long()] = 2.0 ** 120
+    bt.pool["v_scale"][bt.table[1, :5].long()] = 0.0                  # blocks of zeros before, and ones of no size behind
+    bt.pool["v"][bt.table[1, :5].long()] = 0
+    check(bt.cuda(), bt.randn(80, 2, x), 0.2, torch.tensor([0, 40, 80], dtype=torch.int32), max_queries=40)

@@ -458,8 +458,10 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
           float inv;
           const float s = query_scale(most, &inv);
           // a negative scale goes into the queries: the largest sum is then the largest score
-          f = most >= 0x7F800000u ? __uint_as_float(0x7FC00000u) : s * fabsf(a.scale * kLog2e);
-          inv = a.scale < 0.f ? -inv : inv;
+          // a row with an infinity or a NaN has scores of NaN where it sees something: through the queries, so that f leaves -inf what it is
+          const bool number = most < 0x7F800000u && fabsf(a.scale) < TQ_INF;
+          f = number ? s * fabsf(a.scale * kLog2e) : 1.f;
+          inv = !number ? __uint_as_float(0x7FC00000u) : (a.scale < 0.f ? -inv : inv);
 #pragma unroll 2
           for (int i = 0; i < D / 8; ++i) {
             float x[8];
@@ -491,8 +493,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
           const int t0 = (first + i) * kKeys, flags = sh.flags[nt & 3];
           const float2 unit = sh.units[nt & 3];
           const bool edge = t0 + kKeys > it.vis_min || (flags & 0xFFFF) != 0;
-          float factor = f * unit.x;
-          if (factor < 1e-30f) factor = 1e-30f;   // keys of zeros: all scores are (nearly) 0, and -inf stays what it is
+          const float factor = fmaxf(f * unit.x, 1e-30f);   // keys of zeros: all scores are (nearly) 0, and -inf stays what it is
           uint32_t v[2][32];
           auto load_half = [&](int half) {
             tc::tmem_ld32(s_col + 64 * half, v[0]);

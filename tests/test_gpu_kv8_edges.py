@@ -1,0 +1,30 @@
+"""Calls of the paged 8-bit KV cache at the edges of what its documentation allows."""
+import math
+
+import pytest
+import torch
+
+import paper_2504_19874_b200 as tq
+from tests import kv8_reference as ref
+from tests.test_gpu_kv8 import DEV, E4M3, I8, Batch, run_attend, workspace
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("x", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("most", [1, 20])                               # either kernel
+def test_rows_that_see_nothing_are_zeros_whatever_the_query(most, x):
+    bt = Batch([3, 40, 64], d=64, page=16, seed=41).cuda()
+    bt.t[2] = -1                                                        # tokens on no page
+    starts = torch.tensor([0, 20, 40, 60], dtype=torch.int32)
+    Q = bt.randn(60, 4, x)
+    Q[0], Q[5, 1, 3], Q[16, 2, 63], Q[45], Q[59, 0, 0] = math.nan, math.inf, -math.inf, math.nan, math.nan
+    Q[18], Q[30, 3, 5] = math.nan, math.inf                             # these see tokens
+    o, z = run_attend(bt, Q, 0.2, starts, max_queries=most)
+    for rows in (slice(0, 17), slice(40, 60)):
+        assert bool((o[rows] == 0).all()) and bool((z[rows] == -math.inf).all())
+    nan = torch.isnan(o).all(-1).cpu()
+    assert torch.equal(nan, torch.isnan(o).any(-1).cpu()) and torch.equal(nan, torch.isnan(z).cpu())
+    want = torch.zeros(60, 4, dtype=torch.bool)
+    want[18], want[30, 3] = True, True
+    assert torch.equal(nan, want)

@@ -490,7 +490,7 @@ __global__ void __launch_bounds__(kThreads, Kernel<T, D, E4M3, NT>::kCtas) atten
           const float x = ex2(s[nt][e] + (mm == -TQ_INF ? 0.f : kLift - mm));
           l[nt][e & 1] += x;
           y[e] = ex2(s[nt][e] + (mw == -TQ_INF ? -TQ_INF : kLift + (lv - mw)));
-          if (!(vs == vs)) y[e] = edge && x == 0.f ? 0.f : vs;   // what a column does not see adds nothing, NaN or not
+          if (!(vs == vs)) y[e] = edge && t0 + n8 + 8 * (e >> 1) >= vis[nt][e & 1] ? 0.f : vs;   // NaN for the columns that see it
         }
 #pragma unroll
         for (int r = 0; r < 2; ++r) {

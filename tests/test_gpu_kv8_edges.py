@@ -28,3 +28,22 @@ def test_rows_that_see_nothing_are_zeros_whatever_the_query(most, x):
     want = torch.zeros(60, 4, dtype=torch.bool)
     want[18], want[30, 3] = True, True
     assert torch.equal(nan, want)
+
+
+@pytest.mark.parametrize("x", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("most", [1, 5, 30])                            # one warp goes through several tiles, or the other kernel
+def test_a_block_of_nan_shows_where_its_weight_is_nothing_too(most, x):
+    """The last page, partly filled, holds NaN values 2^-200 in weight."""
+    bt = Batch([70] * 130, heads=4, d=32, page=64, seed=6)
+    for row in bt.table.tolist():
+        bt.pool["k"][row[1]] = -64
+        bt.pool["k_scale"][row[1]] = 2.0 ** -6
+        bt.pool["v_scale"][row[1], 1] = math.nan
+    rows = 30 if most == 30 else 1
+    Q = torch.full((130 * rows, 4, 32), 5.0).to(x)
+    starts = torch.arange(0, 131, dtype=torch.int32) * rows
+    o, _ = run_attend(bt.cuda(), Q, 1.0, starts, max_queries=most)
+    nan = torch.isnan(o).view(130, rows, 4, 32).cpu()
+    want = torch.zeros_like(nan)
+    want[:, -6:, 1] = True                                              # the last six rows see tokens 64 and on
+    assert torch.equal(nan, want)

@@ -463,6 +463,11 @@ int tq_kv8_attend(const tq_kv8* cache, const int32_t* table, int64_t ldt, int wi
                   float scale, const int32_t* lists, int nlist, void* out, int64_t ldo, int64_t ho, float* lse, void* workspace,
                   size_t workspace_bytes, void* stream);
 
+/* A wait inside the kernel for many queries is bounded, as everywhere in this library; there is no plan to report it, so the rows that
+ * a broken pipeline leaves undone are NaN in out and lse, never what was there before.
+ * tq_selftest_kv8_timeout, for test suites: while `on` (a switch of the whole process), that kernel's waits run out at once. */
+int tq_selftest_kv8_timeout(int on);
+
 /* The k pages with the best scores for every row and KV head, for tq_kv8_attend's lists: ascending page numbers, -1 behind them where
  * the row sees fewer pages.  With qi = round(q / 2^e) in -127 .. 127 (2^e as for a block), B+ and B- the bounds in steps u s,
  *     score(page) = max over the group's heads of 2^e u s sum_c (max(qi_c, 0) B+_c + min(qi_c, 0) B-_c),

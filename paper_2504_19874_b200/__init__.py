@@ -13,5 +13,5 @@ from .binding import (  # noqa: F401
     KvGroup, tq_attend_decode, tq_attend_decode_workspace_bytes, tq_kv_append,
     TQ_E4M3, TQ_I8, Kv8, Kv8Cache, tq_kv8_append, tq_kv8_attend, tq_kv8_attend_workspace_bytes, tq_kv8_select,
     tq_kv8_select_workspace_bytes, tq_pages_compact, tq_pages_copy, tq_pages_extend, tq_pages_fork, tq_pages_free,
-    tq_pages_workspace_bytes,
+    tq_pages_workspace_bytes, tq_selftest_kv8_timeout,
 )

@@ -73,6 +73,7 @@ _SIGNATURES = {
     "tq_kv8_attend_workspace_bytes": (c_size_t, [c_void_p, c_int, c_int64, c_int, c_int, c_int]),
     "tq_kv8_attend": (c_int, [c_void_p, c_void_p, c_int64, c_int, c_int, c_void_p, c_void_p, c_int64, c_int, c_void_p, c_int64, c_int64, c_int,
                               c_int, ctypes.c_float, c_void_p, c_int, c_void_p, c_int64, c_int64, c_void_p, c_void_p, c_size_t, c_void_p]),
+    "tq_selftest_kv8_timeout": (c_int, [c_int]),
     "tq_kv8_select_workspace_bytes": (c_size_t, [c_void_p, c_int64, c_int]),
     "tq_kv8_select": (c_int, [c_void_p, c_void_p, c_int64, c_int, c_int, c_void_p, c_void_p, c_int64, c_void_p, c_int64, c_int64, c_int, c_int,
                               c_int, c_int, c_int, c_void_p, c_void_p, c_size_t, c_void_p]),
@@ -389,6 +390,11 @@ def tq_kv8_attend(cache: Kv8Cache, table, tokens, Q, scale: float, out, workspac
     if max_queries is None:
         max_queries = 1 if starts is None else Q.shape[0]
     _check((_n or _native()).kv8_attend(cache, table, tokens, starts, Q, scale, out, lse, max_queries, lists, workspace))
+
+
+def tq_selftest_kv8_timeout(on: bool) -> None:
+    """While on, for the whole process, waits of the kernel for many queries run out at once: its rows must be NaN."""
+    _check(lib().tq_selftest_kv8_timeout(int(on)))
 
 
 def tq_kv8_select_workspace_bytes(cache: Kv8Cache, n: int, width: int) -> int:

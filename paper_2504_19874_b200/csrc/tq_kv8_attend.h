@@ -33,6 +33,7 @@ struct AttendArgs {
   float *part_ml, *part_o;   // parts of items: maxima and sums, and outputs divided by these sums
   int pitch;              // columns of a part
   float lift;             // of its weights
+  int give_up;            // (many-query kernel) self test of a wait that runs out
 };
 
 // The many-query kernel (tq_kv8_prompt.cu): workspace beside the few-query kernel's, and its launch, which is followed by the join.

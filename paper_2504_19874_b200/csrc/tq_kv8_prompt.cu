@@ -14,7 +14,7 @@
 // parts that the join kernel adds up.
 // Warps: two groups of four for the softmax of a row tile each (a thread per row, no shuffles), four and three that expand keys and values
 // from global memory through registers into the operand layout, one that issues the MMAs.  While one group works on its S, the tensor cores work for the
-// other.  Waits are bounded; a CTA that gives up writes NaN.
+// other.  Waits are bounded; a CTA that gives one up writes NaN for the item in hand and for the rest of its run.
 //
 // Measured, one B200: 2,048 queries x 32 heads (4 per KV head, d = 128, bf16) over 16,384 tokens 558 us = 924 TFLOP/s, 0.57 of cuBLAS; fp32
 // (four times the MMAs) 1,225 us; a prompt of 4,096 tokens 366 us.  A tile of 128 keys takes about 4,700 cycles, its MMAs 2,050 of them
@@ -33,6 +33,8 @@
 namespace tq {
 namespace kv8 {
 namespace {
+
+std::atomic<int> give_up{0};   // of tq_selftest_kv8_timeout
 
 // Four warps per scheduler, 128 registers each: 8 for the softmax, 4 that expand keys, 3 that expand values, 1 for the MMAs.
 constexpr int kThreads = 512, kExpandWarp0 = 8, kKeyWarps = 4, kValueWarps = 3, kMmaWarp = 15;
@@ -641,6 +643,35 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
         if (lane == 0 && u < u_end) next_item(a, ROWS, &it);
         __syncwarp();
       }
+      while (u < u_end) {                   // a wait has run out: no row is left as it was
+        const int n = min(u_end, item_at + it.tiles) - u, row = tile * 128 + r;
+        const float nan = __uint_as_float(0x7FC00000u);
+        const bool whole = u == item_at && u + n == item_at + it.tiles;
+        if (row < it.cols) {
+          const int c = it.col0 + row, q_head = it.head * a.g + c % a.g;
+          const int64_t q_row = it.row0 + c / a.g;
+          if (whole) {
+            T* out = static_cast<T*>(a.out) + q_row * a.ldo + (int64_t)q_head * a.ho;
+#pragma unroll 1
+            for (int e = 0; e < D; ++e) store_out<T>(out + e, nan);
+            if (a.lse) a.lse[q_row * ((int64_t)a.c.heads * a.g) + q_head] = nan;
+          } else {                          // a sum of NaN makes the joined row NaN
+            a.part_ml[(int64_t)(2 * (int)blockIdx.x + (u == item_at ? 1 : 0)) * 2 * a.pitch + a.pitch + row] = nan;
+          }
+        }
+        if (!whole && u == item_at && t == 0) {
+          meta->row0 = it.row0;
+          meta->col0 = it.col0;
+          meta->cols = it.cols;
+          meta->head = it.head;
+          meta->last_cta = (item_at + it.tiles - 1) / per;
+        }
+        u += n;
+        item_at += it.tiles;
+        __syncwarp();
+        if (lane == 0 && u < u_end) next_item(a, ROWS, &it);
+        __syncwarp();
+      }
     } else if (warp >= kExpandWarp0 && warp < kMmaWarp) {
       // ================================================================ codes -> fp16 operands
       const bool isv = warp >= kExpandWarp0 + kKeyWarps;
@@ -759,6 +790,10 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
     } else if (warp == kMmaWarp && lane == 0) {
       // ================================================================ MMAs
       constexpr uint32_t id_s = idesc_f16(kKeys, false), id_o = idesc_f16(D, true);
+      if (a.give_up) {                      // self test: nothing is issued, so that every wait for it runs out
+        sh.abort_flag = 1;
+        ok = false;
+      }
       const uint32_t q_at = tc::smem_u32(q_sm), k_at = tc::smem_u32(k_sm), v_at = tc::smem_u32(v_sm);
       auto scores = [&](int tile, int st) {
 #pragma unroll
@@ -873,6 +908,7 @@ cudaError_t launch_prompt(AttendArgs& a, int dtype, bool e4m3, int sms, void* wo
   a.part_o = reinterpret_cast<float*>(w + s.o);
   a.pitch = kPromptRows;
   a.lift = dtype == TQ_F32 ? Range<float>::kLift : Range<__nv_bfloat16>::kLift;
+  a.give_up = give_up.load(std::memory_order_relaxed);
   int* status = reinterpret_cast<int*>(w + s.status);   // only written: a CTA whose wait ran out says so with NaN
   const cudaError_t e = dtype == TQ_F32 ? launch_t<float>(a, e4m3, status, sms, st) : launch_t<__nv_bfloat16>(a, e4m3, status, sms, st);
   if (e != cudaSuccess) return e;
@@ -881,3 +917,8 @@ cudaError_t launch_prompt(AttendArgs& a, int dtype, bool e4m3, int sms, void* wo
 
 }  // namespace kv8
 }  // namespace tq
+
+extern "C" int tq_selftest_kv8_timeout(int on) {
+  tq::kv8::give_up.store(on != 0, std::memory_order_relaxed);
+  return TQ_OK;
+}

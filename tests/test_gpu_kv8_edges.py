@@ -47,3 +47,25 @@ def test_a_block_of_nan_shows_where_its_weight_is_nothing_too(most, x):
     want = torch.zeros_like(nan)
     want[:, -6:, 1] = True                                              # the last six rows see tokens 64 and on
     assert torch.equal(nan, want)
+
+
+@pytest.mark.parametrize("x", [torch.bfloat16, torch.float32])
+def test_a_wait_that_runs_out_leaves_no_old_results(x):
+    """Several items per CTA, items that CTAs share, and sequences of few rows, which are the other kernel's."""
+    lens = [400, 300, 50, 200] * 20
+    bt = Batch(lens, heads=2, d=64, page=32, seed=12).cuda()
+    rows = [150, 40, 1, 30] * 20
+    starts = torch.tensor([0] + rows).cumsum(0).to(torch.int32)
+    Q = bt.randn(int(starts[-1]), 4, x)
+    want, lse = run_attend(bt, Q, 0.2, starts, max_queries=150)
+    try:
+        tq.tq_selftest_kv8_timeout(True)
+        o, z = run_attend(bt, Q, 0.2, starts, max_queries=150)
+    finally:
+        tq.tq_selftest_kv8_timeout(False)
+    many = torch.tensor(rows).repeat_interleave(torch.tensor(rows)) > 1
+    assert bool(torch.isnan(o[many]).all()) and bool(torch.isnan(z[many]).all())
+    assert torch.equal(o[~many], want[~many]) and torch.equal(z[~many], lse[~many])
+    assert bool(torch.isfinite(want).all())
+    o, z = run_attend(bt, Q, 0.2, starts, max_queries=150)
+    assert torch.equal(o, want) and torch.equal(z, lse)

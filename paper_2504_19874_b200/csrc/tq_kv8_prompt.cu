@@ -311,6 +311,41 @@ __device__ __forceinline__ void place(int i, int l, int* row, int* chunk) {
   }
 }
 
+// A wait has run out: NaN for the softmax thread's row of every item from unit u on.  Out of line, as it hardly ever runs.
+template <typename T, int D>
+__device__ __noinline__ void rest_is_nan(const AttendArgs& a, Item& it, int u, int u_end, int item_at, int per, int row) {
+  const float nan = __uint_as_float(0x7FC00000u);
+  while (u < u_end) {
+    const int n = min(u_end, item_at + it.tiles) - u;
+    const bool whole = u == item_at && u + n == item_at + it.tiles;
+    if (row < it.cols) {
+      const int c = it.col0 + row, q_head = it.head * a.g + c % a.g;
+      const int64_t q_row = it.row0 + c / a.g;
+      if (whole) {
+        T* out = static_cast<T*>(a.out) + q_row * a.ldo + (int64_t)q_head * a.ho;
+#pragma unroll 1
+        for (int e = 0; e < D; ++e) store_out<T>(out + e, nan);
+        if (a.lse) a.lse[q_row * ((int64_t)a.c.heads * a.g) + q_head] = nan;
+      } else {                              // a sum of NaN makes the joined row NaN
+        a.part_ml[(int64_t)(2 * (int)blockIdx.x + (u == item_at ? 1 : 0)) * 2 * a.pitch + a.pitch + row] = nan;
+      }
+    }
+    if (!whole && u == item_at && row == 0) {
+      Meta* meta = a.meta + blockIdx.x;
+      meta->row0 = it.row0;
+      meta->col0 = it.col0;
+      meta->cols = it.cols;
+      meta->head = it.head;
+      meta->last_cta = (item_at + it.tiles - 1) / per;
+    }
+    u += n;
+    item_at += it.tiles;
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0 && u < u_end) next_item(a, Shape<T, D>::kRows, &it);
+    __syncwarp();
+  }
+}
+
 template <typename T, int D, bool E4M3>
 __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_constant__ AttendArgs a, int* status) {
   using S = Shape<T, D>;
@@ -643,35 +678,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
         if (lane == 0 && u < u_end) next_item(a, ROWS, &it);
         __syncwarp();
       }
-      while (u < u_end) {                   // a wait has run out: no row is left as it was
-        const int n = min(u_end, item_at + it.tiles) - u, row = tile * 128 + r;
-        const float nan = __uint_as_float(0x7FC00000u);
-        const bool whole = u == item_at && u + n == item_at + it.tiles;
-        if (row < it.cols) {
-          const int c = it.col0 + row, q_head = it.head * a.g + c % a.g;
-          const int64_t q_row = it.row0 + c / a.g;
-          if (whole) {
-            T* out = static_cast<T*>(a.out) + q_row * a.ldo + (int64_t)q_head * a.ho;
-#pragma unroll 1
-            for (int e = 0; e < D; ++e) store_out<T>(out + e, nan);
-            if (a.lse) a.lse[q_row * ((int64_t)a.c.heads * a.g) + q_head] = nan;
-          } else {                          // a sum of NaN makes the joined row NaN
-            a.part_ml[(int64_t)(2 * (int)blockIdx.x + (u == item_at ? 1 : 0)) * 2 * a.pitch + a.pitch + row] = nan;
-          }
-        }
-        if (!whole && u == item_at && t == 0) {
-          meta->row0 = it.row0;
-          meta->col0 = it.col0;
-          meta->cols = it.cols;
-          meta->head = it.head;
-          meta->last_cta = (item_at + it.tiles - 1) / per;
-        }
-        u += n;
-        item_at += it.tiles;
-        __syncwarp();
-        if (lane == 0 && u < u_end) next_item(a, ROWS, &it);
-        __syncwarp();
-      }
+      if (!ok) rest_is_nan<T, D>(a, it, u, u_end, item_at, per, tile * 128 + r);
     } else if (warp >= kExpandWarp0 && warp < kMmaWarp) {
       // ================================================================ codes -> fp16 operands
       const bool isv = warp >= kExpandWarp0 + kKeyWarps;

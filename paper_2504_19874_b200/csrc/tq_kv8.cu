@@ -74,6 +74,70 @@ __device__ __forceinline__ void load8(const T* p, bool vec, float (&x)[8]) {
   }
 }
 
+// Four codes as signed bytes in the order of their values (e4m3: sign and magnitude become two's complement, less one), and back.
+template <bool E4M3>
+__device__ __forceinline__ uint32_t ordered(uint32_t w) {
+  return E4M3 ? w ^ ((w & 0x80808080u) >> 7) * 0x7Fu : w;
+}
+__device__ __forceinline__ uint32_t max16(uint32_t a, uint32_t b) {
+  asm("max.s16x2 %0, %0, %1;" : "+r"(a) : "r"(b));
+  return a;
+}
+__device__ __forceinline__ uint32_t min16(uint32_t a, uint32_t b) {
+  asm("min.s16x2 %0, %0, %1;" : "+r"(a) : "r"(b));
+  return a;
+}
+// Largest and smallest code of each channel of a block's first n rows, as ordered bytes: lane l < d / 16 of the warp has channels 16 l to
+// 16 l + 15.  Bytes are compared as the upper halves of 16-bit numbers, two at a time in one instruction.
+template <bool E4M3>
+__device__ __forceinline__ void extremes(const uint8_t* codes, int d, int n, uint32_t (&hi)[4], uint32_t (&lo)[4]) {
+  const int lane = threadIdx.x & 31, cpr = d >> 4, rows = 32 / cpr, chunk = lane % cpr;
+  constexpr int U = 8;                      // rows that a lane asks for at once
+  uint32_t h[8], l[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    h[j] = 0x80008000u;
+    l[j] = 0x7F007F00u;
+  }
+  const uint8_t* from = codes + (lane / cpr) * d + 16 * chunk;
+  const int mine = lane < rows * cpr ? n - lane / cpr : 0;    // rows from this lane's first one on
+#pragma unroll 1
+  for (int r = 0; r < n; r += U * rows) {
+    uint4 w[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i)             // behind the last one: this lane's first row of these again
+      if (r < mine) w[i] = *reinterpret_cast<const uint4*>(from + (r + i * rows < mine ? r + i * rows : r) * d);
+    if (r < mine) {
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        const uint32_t x[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t y = ordered<E4M3>(x[j]), odd = y & 0xFF00FF00u, even = (y << 8) & 0xFF00FF00u;
+          h[2 * j] = max16(h[2 * j], even);
+          h[2 * j + 1] = max16(h[2 * j + 1], odd);
+          l[2 * j] = min16(l[2 * j], even);
+          l[2 * j + 1] = min16(l[2 * j + 1], odd);
+        }
+      }
+    }
+  }
+  for (int s = rows / 2, left = rows; left > 1; left -= s, s = left / 2)   // the last s groups of rows join the first s
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t a = __shfl_down_sync(0xffffffffu, h[j], (left - s) * cpr), b = __shfl_down_sync(0xffffffffu, l[j], (left - s) * cpr);
+      if (lane < s * cpr) {
+        h[j] = max16(h[j], a);
+        l[j] = min16(l[j], b);
+      }
+    }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    hi[j] = h[2 * j] >> 8 | h[2 * j + 1];
+    lo[j] = l[2 * j] >> 8 | l[2 * j + 1];
+  }
+}
+
 // Which (sequence, page) a slot is: the pages that new tokens fall on, sequence after sequence.  One warp looks it up.
 __device__ __forceinline__ void find_slot(const AppendArgs& a, int64_t slot, int lane, int* seq, int64_t* page) {
   int64_t before = 0;
@@ -108,8 +172,8 @@ __device__ __forceinline__ void find_slot(const AppendArgs& a, int64_t slot, int
 // One CTA quantises the new tokens of one page and head, keys (blockIdx.z = 0) or values (1): it alone knows the block's largest
 // magnitude, and old codes of the page are requantised where the scale grows.  NV vectors of 8 channels per thread hold what is new,
 // so the input is read once.  A page per CTA, and not a row: the scale of the page needs all of its new rows at once.  Prompts are bound
-// by the input's bytes behind each CTA's chain of dependent loads (lengths, table, rows): 109 MB in 30 us, 3.6 TB/s; one token each of
-// 128 sequences by that chain alone, 3.4 us.
+// by the input's bytes behind each CTA's chain of dependent loads (lengths, table, rows): 109 MB in 32 us, 3.4 TB/s; one token each of
+// 128 sequences by that chain alone, 4.3 us, 0.8 of it for the old codes of the pages, whose bounds are taken anew.
 template <typename T, bool E4M3, int NV, int NT>
 __global__ void __launch_bounds__(NT) append_kernel(const __grid_constant__ AppendArgs a) {
   __shared__ int found_seq;
@@ -168,6 +232,10 @@ __global__ void __launch_bounds__(NT) append_kernel(const __grid_constant__ Appe
 #pragma unroll
     for (int j = 0; j < 8; ++j) most = max(most, __float_as_uint(v[i][j]) & 0x7FFFFFFFu);
   }
+  // Bounds are those of the codes that count, the old ones among them (what is stored may hold tokens that were taken back).  One token
+  // each: read here, while the new rows are on their way.
+  uint32_t old_hi[4], old_lo[4];
+  if (NT == 32) extremes<E4M3>(codes, d, bounds ? p0 : 0, old_hi, old_lo);
   most = __reduce_max_sync(0xffffffffu, most);
   __syncthreads();
   if (lane == 0) atomicMax(&top, most);
@@ -178,13 +246,12 @@ __global__ void __launch_bounds__(NT) append_kernel(const __grid_constant__ Appe
   else s1 = fmaxf(s0, block_scale<E4M3>(most));
   const float inv = block_inverse(s1), ratio = s0 * inv;
   const bool grown = p0 > 0 && s1 == s1 && s1 != s0;
-  // One token into blocks whose scale holds it: its lanes have a channel each to themselves, and the stored bounds suffice.
+  // One token into blocks whose scale holds it: its lanes have a channel each to themselves.
   const bool one = NT == 32 && !grown;
   if (bounds && !one) {
     for (int c = t; c < d; c += NT) {
-      const bool keep = p0 > 0 && !grown;
-      hi[c] = keep ? bounds[c] : -128;
-      lo[c] = keep ? bounds[d + c] : 127;
+      hi[c] = -128;
+      lo[c] = 127;
     }
     __syncthreads();
   }
@@ -194,16 +261,27 @@ __global__ void __launch_bounds__(NT) append_kernel(const __grid_constant__ Appe
     if (u > hi[ch]) atomicMax(&hi[ch], u);
     if (w < lo[ch]) atomicMin(&lo[ch], w);
   };
-  if (grown) {
+  if (grown || (bounds && !one)) {
     for (int e = t; e < p0 * d / 4; e += NT) {
       uint32_t w = reinterpret_cast<uint32_t*>(codes)[e], o = 0u;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const uint8_t c = encode<E4M3>(decode<E4M3>((uint8_t)(w >> (8 * j))) * ratio);
+        uint8_t c = (uint8_t)(w >> (8 * j));
+        if (grown) c = encode<E4M3>(decode<E4M3>(c) * ratio);
         o |= (uint32_t)c << (8 * j);
         if (bounds) bound((4 * e + j) % d, c);
       }
-      reinterpret_cast<uint32_t*>(codes)[e] = o;
+      if (grown) reinterpret_cast<uint32_t*>(codes)[e] = o;
+    }
+  }
+  uint32_t near_hi[2], near_lo[2];              // old extremes of the 8 channels of this lane's new code
+  if (NT == 32) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const uint32_t a = __shfl_sync(0xffffffffu, old_hi[j], t >> 1), b = __shfl_sync(0xffffffffu, old_hi[2 + j], t >> 1);
+      const uint32_t c = __shfl_sync(0xffffffffu, old_lo[j], t >> 1), e = __shfl_sync(0xffffffffu, old_lo[2 + j], t >> 1);
+      near_hi[j] = t & 1 ? b : a;
+      near_lo[j] = t & 1 ? e : c;
     }
   }
   // A block that reads as NaN gets zeros.  Rounding keeps order, so the bounds of a channel's codes are the codes of its largest and
@@ -231,23 +309,24 @@ __global__ void __launch_bounds__(NT) append_kernel(const __grid_constant__ Appe
       if (bounds && one) {
         uint2* at = reinterpret_cast<uint2*>(bounds + ch);
         uint2* under = reinterpret_cast<uint2*>(bounds + d + ch);
-        const uint2 h = p0 > 0 ? *at : make_uint2(0x80808080u, 0x80808080u), g = p0 > 0 ? *under : make_uint2(0x7F7F7F7Fu, 0x7F7F7F7Fu);
-        uint32_t up[2] = {o.x, o.y}, down[2] = {o.x, o.y};   // int8: a code bounds itself
-        if (E4M3) {
+        uint32_t up[2], down[2];                           // int8: a code bounds itself
 #pragma unroll
-          for (int w = 0; w < 2; ++w) {
-            const uint32_t c = w ? o.y : o.x;
+        for (int w = 0; w < 2; ++w) {
+          const uint32_t c = ordered<E4M3>(w ? o.y : o.x);
+          up[w] = ordered<E4M3>(__vmaxs4(c, near_hi[w]));
+          down[w] = ordered<E4M3>(__vmins4(c, near_lo[w]));
+          if (E4M3) {
+            const uint32_t x = up[w], y = down[w];
             up[w] = down[w] = 0u;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-              const float f = decode<E4M3>((uint8_t)(c >> (8 * j))) * 0.25f;
-              up[w] |= (uint32_t)(uint8_t)__float2int_ru(f) << (8 * j);
-              down[w] |= (uint32_t)(uint8_t)__float2int_rd(f) << (8 * j);
+              up[w] |= (uint32_t)(uint8_t)__float2int_ru(decode<E4M3>((uint8_t)(x >> (8 * j))) * 0.25f) << (8 * j);
+              down[w] |= (uint32_t)(uint8_t)__float2int_rd(decode<E4M3>((uint8_t)(y >> (8 * j))) * 0.25f) << (8 * j);
             }
           }
         }
-        *at = make_uint2(__vmaxs4(h.x, up[0]), __vmaxs4(h.y, up[1]));
-        *under = make_uint2(__vmins4(g.x, down[0]), __vmins4(g.y, down[1]));
+        *at = make_uint2(up[0], up[1]);
+        *under = make_uint2(down[0], down[1]);
       } else if (bounds && !aligned) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) bound(ch + j, (uint8_t)((j < 4 ? o.x : o.y) >> (8 * (j & 3))));

@@ -6,7 +6,7 @@ import torch
 
 import paper_2504_19874_b200 as tq
 from tests import kv8_reference as ref
-from tests.test_gpu_kv8 import DEV, E4M3, I8, Batch, run_attend, workspace
+from tests.test_gpu_kv8 import DEV, E4M3, I8, Batch, check_append, run_attend, workspace
 
 pytestmark = pytest.mark.gpu
 
@@ -69,3 +69,20 @@ def test_a_wait_that_runs_out_leaves_no_old_results(x):
     assert bool(torch.isfinite(want).all())
     o, z = run_attend(bt, Q, 0.2, starts, max_queries=150)
     assert torch.equal(o, want) and torch.equal(z, lse)
+
+
+@pytest.mark.parametrize("dtype", [I8, E4M3])
+@pytest.mark.parametrize("x", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("page,d", [(16, 96), (32, 32), (64, 64), (128, 128), (16, 128), (128, 96)])
+def test_bounds_forget_tokens_that_were_taken_back(page, d, x, dtype):
+    """Drafted tokens, large ones among them, are rejected (the lengths go back) and others appended: bounds are those of the codes that count."""
+    lens = [0, 1, 5, page - 7, page // 2, page - 3, 2 * page - 9]
+    n = len(lens)
+    bt = Batch(lens, heads=3, d=d, page=page, dtype=dtype, seed=page + d, room=2).cuda()
+    before = bt.tokens.clone()
+    starts = torch.arange(0, n + 1, dtype=torch.int32) * 5
+    check_append(bt, before, 1.9 * bt.randn(5 * n, 3, x), bt.randn(5 * n, 3, x), starts)
+    check_append(bt, before + 2, bt.randn(n, 3, x), bt.randn(n, 3, x))                                   # one token each
+    check_append(bt, before + 1, bt.randn(2 * n, 3, x), bt.randn(2 * n, 3, x), torch.arange(0, n + 1, dtype=torch.int32) * 2)
+    check_append(bt, before, 30.0 * bt.randn(n, 3, x), bt.randn(n, 3, x))                                # scales grow
+    check_append(bt, before, 0.1 * bt.randn(n, 3, x), bt.randn(n, 3, x))

@@ -486,7 +486,9 @@ int tq_kv8_select(const tq_kv8* cache, const int32_t* table, int64_t ldt, int wi
  *   spare      device int32 out: free pages left; negative: so many were missing, and the last requests' entries are -1
  *   workspace  256-byte aligned, >= tq_pages_workspace_bytes(pages, rows) (extend), (pages, count) (fork), (pages, 0) (compact)
  *
- * extend   gives row b the pages that next[b] tokens need beyond those of tokens[b] (up to its width; next <= tokens: none)
+ * extend   gives row b the pages that next[b] tokens need beyond those of tokens[b] (up to its width; next <= tokens: none).  Entries
+ *          from there on that hold a page still, up to the first that does not, are kept and none is taken for them: a sequence may be shortened
+ *          (drafted tokens rejected: lower tokens[b]), and a call on a pool that was too small made again
  * fork     makes row children[f] a copy of row parents[f]: its full pages are shared, the page that its last tokens fill in part is
  *          copied to one of the child's own; tokens[child] = tokens[parent].  Children are free rows (what they held is overwritten),
  *          all different and none of them a parent; a parent may have several.  Row numbers outside the table are passed over

@@ -29,18 +29,25 @@ struct TakeArgs {
   const int32_t* next;       // extend: lengths to have room for; fork: NULL
   const int32_t *parents, *children;
   int units, page_shift;     // requests: sequences (extend) or children (fork)
-  int32_t *counts, *offsets, *fresh;   // workspace: free pages of each chunk, first request of each unit, page of each child
+  int32_t *counts, *offsets;           // workspace: free pages of each chunk, first request of each unit
+  int32_t* fresh;                      // ... and first entry to fill of each sequence (extend), page of each child (fork)
   int32_t* spare;
 };
 
-// Pages that unit u asks for.  *first: extend: the first entry of its row without one; fork: the parent's page to copy.
+// Pages that unit u asks for.  *first: extend: the first entry of its row without one, behind those that a sequence that was shortened,
+// or that a pool ran short for, still has (read before any entry is filled); fork: the parent's page to copy.
 __device__ __forceinline__ int asked(const TakeArgs& a, int u, int* first) {
   const int T1 = (1 << a.page_shift) - 1;
   if (a.next != nullptr) {
     const int64_t have = ((int64_t)max(a.t.tokens[u], 0) + T1) >> a.page_shift;
     const int64_t need = min(((int64_t)max(a.next[u], 0) + T1) >> a.page_shift, (int64_t)a.t.width);
-    *first = (int)min(have, (int64_t)a.t.width);
-    return need > have ? (int)(need - have) : 0;
+    int64_t j = have;
+    for (; j < need; ++j) {
+      const int id = a.t.table[(int64_t)u * a.t.ldt + j];
+      if (id < 0 || id >= a.pages || a.refs[id] <= 0) break;
+    }
+    *first = (int)min(j, (int64_t)a.t.width);
+    return need > j ? (int)(need - j) : 0;
   }
   *first = 0;
   const int p = a.parents[u], c = a.children[u];
@@ -100,7 +107,10 @@ __global__ void __launch_bounds__(kThreads) count_kernel(const __grid_constant__
     int first;
     const int n = u0 + t < a.units ? asked(a, u0 + t, &first) : 0;
     const int upto = block_sum_upto(n, warp_sums, &total);
-    if (u0 + t < a.units) a.offsets[u0 + t] = before + upto - n;
+    if (u0 + t < a.units) {
+      a.offsets[u0 + t] = before + upto - n;
+      if (a.next != nullptr) a.fresh[u0 + t] = first;
+    }
     before += total;
   }
   if (t == 0) a.offsets[a.units] = before;
@@ -114,9 +124,7 @@ __device__ __forceinline__ void give(const TakeArgs& a, int r, int id) {
     if (a.offsets[mid] <= r) lo = mid; else hi = mid - 1;
   }
   if (a.next != nullptr) {
-    int first;
-    asked(a, lo, &first);
-    a.t.table[(int64_t)lo * a.t.ldt + first + (r - a.offsets[lo])] = id;
+    a.t.table[(int64_t)lo * a.t.ldt + a.fresh[lo] + (r - a.offsets[lo])] = id;
   } else {
     a.fresh[lo] = id;
   }
@@ -171,7 +179,10 @@ __global__ void __launch_bounds__(kThreads) take_small_kernel(const __grid_const
     int first;
     const int n = u0 + t < a.units ? asked(a, u0 + t, &first) : 0;
     const int upto = block_sum_upto(n, warp_sums, &total);
-    if (u0 + t < a.units) a.offsets[u0 + t] = wanted + upto - n;
+    if (u0 + t < a.units) {
+      a.offsets[u0 + t] = wanted + upto - n;
+      if (a.next != nullptr) a.fresh[u0 + t] = first;
+    }
     wanted += total;
   }
   if (t == 0) a.offsets[a.units] = wanted;

@@ -182,3 +182,43 @@ def test_a_captured_step_follows_the_state():
         assert spare.item() == pages - held and int(refs.sum()) == held
         used = table[table >= 0]
         assert used.numel() == held == used.unique().numel()
+
+
+@pytest.mark.parametrize("pages", [40, 9001])                          # one launch, and two
+def test_extending_a_shortened_sequence_keeps_its_pages(pages):
+    st = State(pages, 3, 12)
+    st.extend([70, 33, 0])
+    held = [list(r) for r in st.table]
+    st.tokens = [40, 33, 0]                                            # 30 drafted tokens rejected: pages 3 and 4 of row 0 stay its own
+    st.d_tokens.copy_(ints(st.tokens))
+    ws = workspace(pages, 3)
+    tq.tq_pages_extend(st.d_refs, st.d_table, st.d_tokens, ints([60, 33, 0]), 16, st.spare, ws)
+    st.check(pages - 8)
+    assert st.table == held
+    tq.tq_pages_extend(st.d_refs, st.d_table, st.d_tokens, ints([100, 49, 16]), 16, st.spare, ws)
+    st.table[0][5:7], st.table[1][3], st.table[2][0] = [8, 9], 10, 11
+    for p in range(8, 12):
+        st.refs[p] = 1
+    st.check(pages - 12)
+    st.tokens = [100, 49, 16]
+    st.d_tokens.copy_(ints(st.tokens))
+    st.free([0, 1, 2])
+    assert st.refs == [0] * pages
+
+
+def test_a_call_on_a_pool_that_was_too_small_made_again():
+    st = State(6, 3, 8)
+    st.extend([33, 0, 0])
+    ws = workspace(6, 3)
+    tq.tq_pages_extend(st.d_refs, st.d_table, st.d_tokens, ints([33, 40, 30]), 16, st.spare, ws)   # three more for row 1, two for row 2: 3 are left
+    assert st.spare.item() == -2 and st.d_table[1:, :3].tolist() == [[3, 4, 5], [-1, -1, -1]]
+    tq.tq_pages_free(st.d_refs, st.d_table, st.d_tokens, ints([0]))
+    tq.tq_pages_extend(st.d_refs, st.d_table, st.d_tokens, ints([0, 40, 30]), 16, st.spare, ws)
+    assert st.spare.item() == 1 and st.d_table[1:, :3].tolist() == [[3, 4, 5], [0, 1, -1]] and st.d_refs.tolist() == [1, 1, 0, 1, 1, 1]
+
+
+def test_entries_of_free_pages_hold_none():
+    st = State(30, 2, 4)
+    st.d_table.fill_(7)                                                # numbers of a page that nobody has
+    tq.tq_pages_extend(st.d_refs, st.d_table, st.d_tokens, ints([40, 20]), 16, st.spare, workspace(30, 2))
+    assert st.d_table.tolist() == [[0, 1, 2, 7], [3, 4, 7, 7]] and st.spare.item() == 25

@@ -450,7 +450,8 @@ int tq_kv8_append(const tq_kv8* cache, const int32_t* table, int64_t ldt, int wi
  * out = 0 and lse = -inf.
  *   Q, out       [n rows, heads * q_per_kv, d] of dtype, row strides ldq / ldo, head strides hq / ho; 1 <= q_per_kv <= 256.
  *                TQ_BF16: weights are rounded to 11 bits; TQ_F32: products as exact as fp32 sums
- *   max_queries  the largest number of rows of a sequence: it chooses the kernels (a wrong figure costs time, not results)
+ *   max_queries  the largest number of rows of a sequence: it chooses the kernels (a wrong figure costs time, not results).  0 and no
+ *                workspace, with `starts`: the caller says that there are no rows, and nothing is done
  *   lists        NULL, or [n, heads, nlist >= 1] int32: the numbers of the pages (entries of the sequence's row of the table) that a row
  *                attends to, shared by the heads of a group, in any order; entries outside the sequence's pages are passed over, a
  *                page that is listed twice counts twice

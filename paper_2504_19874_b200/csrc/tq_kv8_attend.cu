@@ -813,7 +813,7 @@ extern "C" size_t tq_kv8_attend_workspace_bytes(const tq_kv8* cache, int nseq, i
   int dev = 0, sms = 0;
   if (cache == nullptr || cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
   (void)nseq; (void)n;
-  const bool many = nlist == 0 && (int64_t)max_queries * q_per_kv > kMaxCols;
+  const bool many = nlist == 0 && (int64_t)std::max(max_queries, 1) * q_per_kv > kMaxCols;
   return attend_space(sms, cache->d) + (many ? prompt_space(sms, cache->d) : 0);
 }
 
@@ -836,7 +836,8 @@ extern "C" int tq_kv8_attend(const tq_kv8* cache, const int32_t* table, int64_t 
   TQ_REQUIRE(starts != nullptr || max_queries >= 1, TQ_ERR_INVALID_ARG, "%s: max_queries is 0 where every sequence has one row", who);
   TQ_REQUIRE((lists != nullptr) == (nlist > 0), TQ_ERR_INVALID_ARG, "%s: lists of %d pages", who, nlist);
   TQ_REQUIRE(nlist <= (1 << 24), TQ_ERR_UNSUPPORTED, "%s: lists of %d pages", who, nlist);
-  if (nseq == 0 || n == 0 || max_queries == 0) return TQ_OK;
+  if (nseq == 0 || n == 0 || (max_queries == 0 && workspace == nullptr)) return TQ_OK;
+  max_queries = std::max(max_queries, 1);   // the figure only chooses kernels: rows that `starts` has all the same are computed
   TQ_REQUIRE(Q != nullptr && out != nullptr, TQ_ERR_INVALID_ARG, "%s: Q or out is NULL", who);
   TQ_REQUIRE(ldq >= 0 && hq >= 0 && ldo >= 0 && ho >= 0, TQ_ERR_INVALID_ARG, "%s: negative stride", who);
   const uintptr_t align = dtype == TQ_F32 ? 3 : 1;

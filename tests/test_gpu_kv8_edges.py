@@ -6,7 +6,7 @@ import torch
 
 import paper_2504_19874_b200 as tq
 from tests import kv8_reference as ref
-from tests.test_gpu_kv8 import DEV, E4M3, I8, Batch, check_append, run_attend, workspace
+from tests.test_gpu_kv8 import DEV, E4M3, I8, Batch, check_append, check_attend, run_attend, workspace
 
 pytestmark = pytest.mark.gpu
 
@@ -86,3 +86,12 @@ def test_bounds_forget_tokens_that_were_taken_back(page, d, x, dtype):
     check_append(bt, before + 1, bt.randn(2 * n, 3, x), bt.randn(2 * n, 3, x), torch.arange(0, n + 1, dtype=torch.int32) * 2)
     check_append(bt, before, 30.0 * bt.randn(n, 3, x), bt.randn(n, 3, x))                                # scales grow
     check_append(bt, before, 0.1 * bt.randn(n, 3, x), bt.randn(n, 3, x))
+
+
+@pytest.mark.parametrize("x", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("g", [3, 20])
+def test_attend_with_a_largest_number_of_rows_of_none(g, x):
+    """The figure is wrong: it costs time, not results."""
+    bt = Batch([90, 20, 64], d=64, page=32, dtype=E4M3, seed=17).cuda()
+    starts = torch.tensor([0, 33, 34, 60], dtype=torch.int32)
+    check_attend(bt, bt.randn(60, 2 * g, x), 0.15, starts, max_queries=0)

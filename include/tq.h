@@ -422,7 +422,8 @@ int tq_entropy_unpack(const tq_plan* plan, const uint8_t* lengths, int64_t n, co
  *
  * The caller owns every array and keeps the lengths: tokens[b] is a device array, read by the kernels, so a captured graph follows it.
  *   table   device int32, one row per sequence, row stride ldt >= width: entry j is the page of tokens j * page_tokens and on; -1 (or
- *           any number outside the pool) is no page: attention passes over its tokens, appended tokens are dropped.
+ *           any number outside the pool) is no page: attention passes over its tokens, appended tokens are dropped.  width is at most
+ *           2^24, and width * page_tokens at most 2^31 - 256.
  *   starts  device int32[nseq + 1], ascending: the rows of Q, K, V and out that belong to sequence b are starts[b] .. starts[b+1] - 1;
  *           NULL: one row per sequence.  Rows behind the last sequence are neither read nor written.
  * d is 32, 64, 96 or 128, page_tokens 16, 32, 64 or 128; row and head strides of Q, K, V and out are in elements and arbitrary (channels are

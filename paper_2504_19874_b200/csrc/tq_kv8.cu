@@ -26,11 +26,13 @@ int check_cache(const char* who, const tq_kv8* c, Cache* out) {
   return TQ_OK;
 }
 
-int check_batch(const char* who, const int32_t* table, int64_t ldt, int width, int nseq, const int32_t* tokens, const int32_t* starts,
-                int64_t n, Batch* out) {
+int check_batch(const char* who, const Cache& c, const int32_t* table, int64_t ldt, int width, int nseq, const int32_t* tokens,
+                const int32_t* starts, int64_t n, Batch* out) {
   TQ_REQUIRE(nseq >= 0 && n >= 0 && width >= 0, TQ_ERR_INVALID_ARG, "%s: negative size", who);
   TQ_REQUIRE(nseq <= (1 << 20) && n < (1ll << 31), TQ_ERR_UNSUPPORTED, "%s: at most 2^20 sequences and 2^31 - 1 rows", who);
   TQ_REQUIRE(width <= (1 << 24), TQ_ERR_UNSUPPORTED, "%s: at most 2^24 pages per sequence", who);
+  TQ_REQUIRE(((int64_t)width << c.page_shift) <= (1ll << 31) - 256, TQ_ERR_UNSUPPORTED, "%s: a table of %d pages holds more than 2^31 - 256 tokens", who,
+             width);   // positions of tokens, and of the ends of the tiles that they lie in, are 32-bit numbers
   TQ_REQUIRE(nseq == 0 || (tokens && (table || width == 0)), TQ_ERR_INVALID_ARG, "%s: page table or lengths are NULL", who);
   TQ_REQUIRE(ldt >= width, TQ_ERR_INVALID_ARG, "%s: row stride %lld of the table is smaller than its width %d", who, (long long)ldt, width);
   TQ_REQUIRE(starts != nullptr || n == nseq, TQ_ERR_INVALID_ARG, "%s: %lld rows for %d sequences without starts (one row each)", who, (long long)n, nseq);
@@ -712,7 +714,7 @@ extern "C" int tq_kv8_append(const tq_kv8* cache, const int32_t* table, int64_t 
   AppendArgs a;
   std::memset(&a, 0, sizeof(a));
   int rc = check_cache(who, cache, &a.c);
-  if (rc == TQ_OK) rc = check_batch(who, table, ldt, width, nseq, tokens, starts, n, &a.b);
+  if (rc == TQ_OK) rc = check_batch(who, a.c, table, ldt, width, nseq, tokens, starts, n, &a.b);
   if (rc != TQ_OK) return rc;
   TQ_REQUIRE(dtype == TQ_F32 || dtype == TQ_BF16, TQ_ERR_UNSUPPORTED, "%s: unknown dtype %d", who, dtype);
   if (nseq == 0 || n == 0 || cache->pages == 0) return TQ_OK;
@@ -752,7 +754,7 @@ extern "C" int tq_kv8_select(const tq_kv8* cache, const int32_t* table, int64_t 
   SelectArgs a;
   std::memset(&a, 0, sizeof(a));
   int rc = check_cache(who, cache, &a.c);
-  if (rc == TQ_OK) rc = check_batch(who, table, ldt, width, nseq, tokens, starts, n, &a.b);
+  if (rc == TQ_OK) rc = check_batch(who, a.c, table, ldt, width, nseq, tokens, starts, n, &a.b);
   if (rc != TQ_OK) return rc;
   TQ_REQUIRE(dtype == TQ_F32 || dtype == TQ_BF16, TQ_ERR_UNSUPPORTED, "%s: unknown dtype %d", who, dtype);
   TQ_REQUIRE(q_per_kv >= 1 && q_per_kv <= 256, TQ_ERR_UNSUPPORTED, "%s: 1..256 queries per KV head", who);

@@ -31,8 +31,8 @@ struct Batch {
 
 // Checks shared by the entry points; fills `out`.  0 or a TQ_ERR_* code.
 int check_cache(const char* who, const tq_kv8* c, Cache* out);
-int check_batch(const char* who, const int32_t* table, int64_t ldt, int width, int nseq, const int32_t* tokens, const int32_t* starts,
-                int64_t n, Batch* out);
+int check_batch(const char* who, const Cache& c, const int32_t* table, int64_t ldt, int width, int nseq, const int32_t* tokens,
+                const int32_t* starts, int64_t n, Batch* out);
 
 #ifdef __CUDACC__
 // First and last row of sequence b, whatever the caller's array says: 0 <= begin <= end <= n.

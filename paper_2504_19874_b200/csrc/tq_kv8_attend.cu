@@ -828,7 +828,7 @@ extern "C" int tq_kv8_attend(const tq_kv8* cache, const int32_t* table, int64_t 
   AttendArgs a;
   std::memset(&a, 0, sizeof(a));
   int rc = check_cache(who, cache, &a.c);
-  if (rc == TQ_OK) rc = check_batch(who, table, ldt, width, nseq, tokens, starts, n, &a.b);
+  if (rc == TQ_OK) rc = check_batch(who, a.c, table, ldt, width, nseq, tokens, starts, n, &a.b);
   if (rc != TQ_OK) return rc;
   TQ_REQUIRE(dtype == TQ_F32 || dtype == TQ_BF16, TQ_ERR_UNSUPPORTED, "%s: unknown dtype %d", who, dtype);
   TQ_REQUIRE(q_per_kv >= 1 && q_per_kv <= 256, TQ_ERR_UNSUPPORTED, "%s: 1..256 queries per KV head", who);

@@ -128,3 +128,12 @@ def test_tensors_of_the_host_are_refused():
         tq.Kv8Cache(k.float(), k.float(), s, s.clone())
     with pytest.raises(ValueError):
         tq.tq_pages_free(torch.zeros(4, dtype=torch.int32), torch.zeros((1, 4), dtype=torch.int32), None, torch.zeros(1, dtype=torch.int32))
+
+
+@pytest.mark.parametrize("call", [append, attend, select])
+def test_tables_of_more_tokens_than_32_bits_count(call):
+    for t in (16, 32, 64, 128):
+        most = min(1 << 24, ((1 << 31) - 256) // t)
+        for width in (most, most + 1):
+            rc = call(cache(page_tokens=t), width=width, ldt=width, n=0)
+            assert rc == (0 if width == most else UNSUPPORTED)

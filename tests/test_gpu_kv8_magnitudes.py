@@ -175,3 +175,13 @@ def test_the_largest_and_no_values_of_prompts(x):
     bt.pool["v_scale"][bt.table[1, :5].long()] = 0.0                  # blocks of zeros before, and ones of no size behind
     bt.pool["v"][bt.table[1, :5].long()] = 0
     check(bt.cuda(), bt.randn(80, 2, x), 0.2, torch.tensor([0, 40, 80], dtype=torch.int32), max_queries=40)
+
+
+@pytest.mark.parametrize("x", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("order", ["down", "spread_50"])
+def test_one_sequence_in_hundreds_of_parts(order, x):
+    bt = Batch([40_000], heads=1, d=32, page=128, seed=8)
+    scale_pages(bt, "v_scale", ORDERS[order], 7)
+    check(bt.cuda(), bt.randn(1, 2, x), 0.2)
+    check(bt, bt.randn(20, 2, x), 0.2, torch.tensor([0, 20], dtype=torch.int32), max_queries=20)
+    check(bt, bt.randn(3, 2, x), 0.2, torch.tensor([0, 3], dtype=torch.int32), max_queries=3)

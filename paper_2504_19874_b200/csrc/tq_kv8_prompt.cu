@@ -6,8 +6,10 @@
 // as two limbs), P is one fp16 limb for bf16 outputs and two for fp32 ones, m is the row's running maximum and r that of s + log2 v, whole
 // numbers that only rise, when a score exceeds one of them by far: then the row's O in TMEM is rescaled by its own thread.  Sums are fp32.
 // v and its like for keys are the tile's units, the largest scales of its blocks.  The codes become fp16 in shared memory times their
-// block's scale over the unit, a power of two from 2^-15 to 1 and so exactly.  Blocks below that are left out (masked, as keys that nobody sees)
-// and take their turn with units of their own in a second pass over the same tile: what one page holds changes nothing for another.
+// block's scale over the unit, a power of two: from 2^-15 to 1 for keys, exactly; from 2^-2 to 1 for values, as r and with it P's smallest
+// step follow the unit for rows too that do not see the block it comes from.  Blocks below that, and values of 0, are left out (masked, as keys
+// that nobody sees) and take their turn with units of their own in a second pass over the same tile: what one page holds changes nothing
+// for another.
 //
 // Work.  A CTA per SM; units are (tile of 128 keys) x (block of 256 rows, fp32: 128), numbered through over blocks, heads and sequences,
 // and every CTA takes an equal run of them, so that causal triangles and ragged batches are even; runs that end inside a block leave
@@ -51,11 +53,13 @@ struct Shape {
   static constexpr uint32_t smem = 6 * kOperand + 1024 + 2048;    // two of queries (row tiles, or limbs), two stages of keys and values
 };
 
-// Weights are 2^(s - m + kLift), and m moves when a score exceeds it by more than kSlack: rescaling O costs about as much as a tile.  fp32
-// outputs keep the few-query kernel's figures; for bf16 ones weights below 2^-17 of the largest may lose bits (2^-28 of it each).
+// Weights are 2^(s - m + kLift), and m moves when a score exceeds it by more than kSlack: rescaling O costs about as much as a tile, and
+// 2^15 is the largest power of two in fp16.  With
+// r up to 2^3 above the row's largest product of weight and scale (a whole number, and the unit of values up to 2^2 larger), what lies
+// below 2^-16 (bf16) or 2^-19 (fp32) of that may lose bits, 2^-27 or 2^-30 of it each.
 template <typename T>
 struct Range {
-  static constexpr float kLift = sizeof(T) == 4 ? 6.f : 3.f, kSlack = sizeof(T) == 4 ? 8.f : 11.f;
+  static constexpr float kLift = sizeof(T) == 4 ? 8.f : 5.f, kSlack = 15.f - kLift;
 };
 
 struct Bars {
@@ -758,11 +762,11 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
         read(now.id, first, raw);
         bool left = true;                   // these keys have not been in a pass
         for (int i = 0; i < n;) {
-          // units of what is left: scales are positive, so their bits are in their order; 0 and NaN go with any unit
+          // units of what is left: scales are positive, so their bits are in their order; keys of 0, and NaN, go with any unit
           const float uk = __uint_as_float(__reduce_max_sync(0xffffffffu, left && now.ks > 0.f ? __float_as_uint(now.ks) : 0u));
           bool in = left && !(now.ks < uk * 0x1p-15f && now.ks > 0.f);
           const float uv = __uint_as_float(__reduce_max_sync(0xffffffffu, in && now.vs > 0.f ? __float_as_uint(now.vs) : 0u));
-          in = in && !(now.vs < uv * 0x1p-15f && now.vs > 0.f);
+          in = in && !(now.vs < uv * 0.25f);
           const bool again = __any_sync(0xffffffffu, left && !in);
           left = left && !in;
           in = in && now.id >= 0;

@@ -29,8 +29,11 @@ def bounded(bt, Q, scale, starts=None, lists=None):
         for h in range(heads):
             pos = torch.arange(seen)
             if lists is not None:
-                pos = torch.cat([torch.arange(j * T, (j + 1) * T) for j in lists[r, h].tolist() if 0 <= j < bt.table.shape[1]])
+                pages = [j for j in lists[r, h].tolist() if 0 <= j < bt.table.shape[1]]
+                pos = (torch.tensor(pages, dtype=torch.long)[:, None] * T + torch.arange(T)).flatten()
                 pos = pos[pos < seen]
+            page = bt.table[b, pos // T]
+            pos = pos[(page >= 0) & (page < bt.pool["k"].shape[0])]
             if not pos.numel():
                 out[r, h * g:(h + 1) * g], lse[r, h * g:(h + 1) * g] = 0.0, -math.inf
                 continue
@@ -185,3 +188,21 @@ def test_one_sequence_in_hundreds_of_parts(order, x):
     check(bt.cuda(), bt.randn(1, 2, x), 0.2)
     check(bt, bt.randn(20, 2, x), 0.2, torch.tensor([0, 20], dtype=torch.int32), max_queries=20)
     check(bt, bt.randn(3, 2, x), 0.2, torch.tensor([0, 3], dtype=torch.int32), max_queries=3)
+
+
+@pytest.mark.parametrize("x", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("dtype", [I8, E4M3])
+@pytest.mark.parametrize("near", [None, 0, 1, 2, 5, 14, 16, 40])
+def test_pages_beside_a_large_one_keep_their_bits(near, dtype, x):
+    """One tile of 128 keys with a large last page, that early rows do not see, and pages 2^near below it, or of zeros (None), that they do;
+    the others are smaller still."""
+    bt = Batch([256], heads=1, d=32, page=16, dtype=dtype, seed=7)
+    p = bt.table[0].tolist()
+    for j in range(16):
+        if j < 8 or 11 <= j < 14:
+            bt.pool["v_scale"][p[j]] *= 2.0 ** -30
+        elif j < 14:
+            bt.pool["v_scale"][p[j]] *= 0.0 if near is None else 2.0 ** (30 - near)
+        else:
+            bt.pool["v_scale"][p[j]] *= 2.0 ** 30
+    check(bt.cuda(), bt.randn(140, 2, x), 0.2, torch.tensor([0, 140], dtype=torch.int32), max_queries=140)

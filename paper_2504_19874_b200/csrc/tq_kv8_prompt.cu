@@ -766,7 +766,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
           const float uk = __uint_as_float(__reduce_max_sync(0xffffffffu, left && now.ks > 0.f ? __float_as_uint(now.ks) : 0u));
           bool in = left && !(now.ks < uk * 0x1p-15f && now.ks > 0.f);
           const float uv = __uint_as_float(__reduce_max_sync(0xffffffffu, in && now.vs > 0.f ? __float_as_uint(now.vs) : 0u));
-          in = in && !(now.vs < uv * 0.25f);
+          in = in && !(now.vs < uv * 0.25f && now.id >= 0);
           const bool again = __any_sync(0xffffffffu, left && !in);
           left = left && !in;
           in = in && now.id >= 0;

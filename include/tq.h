@@ -407,8 +407,8 @@ int tq_entropy_unpack(const tq_plan* plan, const uint8_t* lengths, int64_t n, co
                       const uint64_t* row_offsets, uint8_t* idx, void* stream);
 
 /* ---------------------------------------------------------------------------------------------
- * Paged 8-bit KV cache: the tokens that 2 to 4 bits are too coarse for (recent tokens, prompts, whole layers), for many sequences
- * at once.  A cache is a pool of pages of page_tokens tokens each, all KV heads in a page; a sequence owns the pages that its row
+ * Paged 8-bit KV cache: layers that 2 to 4 bits are too coarse for, prompts, drafted tokens, for many sequences at once.  A layer's
+ * tokens of a sequence are all in such a cache or all in the compressed one above: no call joins attention over both.  A cache is a pool of pages of page_tokens tokens each, all KV heads in a page; a sequence owns the pages that its row
  * of a page table names.  A block is one page of one head: its keys have one scale, its values another.
  *
  *   scale   s = 2^e with the least e >= -126 that holds the block's largest magnitude: max |x| <= M 2^e, M = 127 (TQ_I8) or 448
@@ -416,6 +416,8 @@ int tq_entropy_unpack(const tq_plan* plan, const uint8_t* lengths, int64_t n, co
  *           an int8 value in -127 .. 127, or the bits of an e4m3 number.  A stored element is code * s.
  *   growth  tokens are added one after another: a later token that the scale does not hold raises it, and the block's codes are
  *           rounded to the new scale (off by at most one step of it in all).  Writing at a page's first slot starts its blocks afresh.
+ *           Tokens may be taken back by a lower tokens[b] (drafts that were rejected): later ones overwrite them, and nothing of them
+ *           is left but the scale.
  *   NaN     a block that is given an infinity or a NaN has scale NaN from then on: all of it reads as NaN, visibly.
  *   bounds  optional: per block and channel the largest and the smallest key code, in steps of 1 (TQ_I8) or, rounded outwards, of 4
  *           (TQ_E4M3) scales.  tq_kv8_select ranks pages by them.
@@ -450,7 +452,9 @@ int tq_kv8_append(const tq_kv8* cache, const int32_t* table, int64_t ldt, int wi
  * the rows are the sequence's last m tokens (tokens counts them), each sees itself and what is before it.  A row that sees nothing has
  * out = 0 and lse = -inf.
  *   Q, out       [n rows, heads * q_per_kv, d] of dtype, row strides ldq / ldo, head strides hq / ho; 1 <= q_per_kv <= 256.
- *                TQ_BF16: weights are rounded to 11 bits; TQ_F32: products as exact as fp32 sums
+ *                TQ_BF16: weights are rounded to 11 bits, and where a weight times its value scale is below 2^-16 of the row's largest such
+ *                product by 2^-27 of that; elements of a row of Q below 2^-30 of its largest lose bits.  TQ_F32: 22 bits, 2^-30 of that, and
+ *                2^-22 of each element.  All sums are fp32.  Pages of very unlike magnitudes cost time at most, not each other's bits
  *   max_queries  the largest number of rows of a sequence: it chooses the kernels (a wrong figure costs time, not results).  0 and no
  *                workspace, with `starts`: the caller says that there are no rows, and nothing is done
  *   lists        NULL, or [n, heads, nlist >= 1] int32: the numbers of the pages (entries of the sequence's row of the table) that a row
@@ -473,8 +477,8 @@ int tq_selftest_kv8_timeout(int on);
 /* The k pages with the best scores for every row and KV head, for tq_kv8_attend's lists: ascending page numbers, -1 behind them where
  * the row sees fewer pages.  With qi = round(q / 2^e) in -127 .. 127 (2^e as for a block), B+ and B- the bounds in steps u s,
  *     score(page) = max over the group's heads of 2^e u s sum_c (max(qi_c, 0) B+_c + min(qi_c, 0) B-_c),
- * for scale > 0 no less than any logit of the page up to q's rounding.  Sums of integers and powers of two: scores are exact, and of
- * equal ones the lower page number is taken.  The first `first` and the last `last` pages that the row sees are always taken
+ * for scale > 0 no less than any logit of the page up to q's rounding.  Sums of integers and powers of two: scores are exact (where they
+ * lie within the normal numbers of fp32), and of equal ones the lower page number is taken.  The first `first` and the last `last` pages that the row sees are always taken
  * (first + last <= k), and so, as far as k goes, is a block with scale NaN.  A query with an infinity or a NaN scores 0 everywhere.
  *   lists      device out, [n, heads, k];  workspace  256-byte aligned, >= tq_kv8_select_workspace_bytes(cache, n, width)
  */
@@ -485,7 +489,8 @@ int tq_kv8_select(const tq_kv8* cache, const int32_t* table, int64_t ldt, int wi
 
 /* Bookkeeping of the pages.  refs[p] (device int32) counts the table rows that hold page p; a page with 0 is free.  Calls take the lowest
  * free pages, in the order of their requests, so the same calls give the same tables.  `rows` rows of the table, as above.
- *   spare      device int32 out: free pages left; negative: so many were missing, and the last requests' entries are -1
+ *   spare      device int32 out: free pages left; negative: so many were missing, and the last requests' entries are -1 (free the children
+ *              of a fork that ran short before it is made again).  A call with nothing to do (no rows, children or pages) leaves it be
  *   workspace  256-byte aligned, >= tq_pages_workspace_bytes(pages, rows) (extend), (pages, count) (fork), (pages, 0) (compact)
  *
  * extend   gives row b the pages that next[b] tokens need beyond those of tokens[b] (up to its width; next <= tokens: none).  Entries

@@ -17,11 +17,11 @@
 // and of a unit each of its four warps takes 16 tokens, through a ring of its own in shared memory, some steps ahead.  Warps are
 // independent until their share of an item ends; items that several CTAs share are joined by a second, dependent launch in a fixed order.
 //
-// Measured, one B200, 8 KV heads x 4 queries, d = 128: 37 sequences of 8,192 tokens stream at 5.0 TB/s, a ragged batch of 64 (563 MB) at
-// 4.9 TB/s (115 us; 0.75 of the copy bandwidth), one sequence of 32,768 tokens 27 us, of which the loop takes 10 us at the copy bandwidth
-// and the chain of first loads, the last sums and the join the rest; 1,000 tokens 9.6 us.  Reading the tiles straight into registers,
+// Measured, one B200, 8 KV heads x 4 queries, d = 128: 37 sequences of 8,192 tokens stream at 5.2 TB/s, a ragged batch of 64 (563 MB) at
+// 4.8 TB/s (118 us; 0.73 of the copy bandwidth), one sequence of 32,768 tokens 28 us, of which the loop takes 10 us at the copy bandwidth
+// and the chain of first loads, the last sums and the join the rest; 1,000 tokens 9.7 us.  Reading the tiles straight into registers,
 // one step ahead, took 228 us for the batch and 43 us for the layer: eight warps per SM had too few bytes on their way.  Long calls
-// are bound by HBM; half of the issue slots and of the ALU pipe, which unpacks the codes, are in use meanwhile.
+// are bound by HBM (63 % of its cycles in the batch's kernel); half of the issue slots are in use meanwhile.
 #include <algorithm>
 #include <cstring>
 
@@ -169,7 +169,7 @@ __global__ void __launch_bounds__(kThreads, Kernel<T, D, E4M3, NT>::kCtas) atten
   // A share that ends one item and begins the next pays for its first loads and last sums twice, about as much as kCross units.  Where
   // there are fewer items than CTAs, shares are therefore laid so that each lies within one item (items count as a multiple of `per`
   // then, the units behind their end being empty), unless that makes them longer by more than that: nine sequences of up to five
-  // tokens 19.8 -> 18.0 us, a head's 32,768 tokens 27.7 -> 27.4, the pages of 24 rows 43.1 -> 42.4.
+  // tokens 19.8 -> 18.0 us, 32,768 tokens 27.7 -> 27.4, the pages of 24 rows 43.1 -> 42.4 (as it was added).
   constexpr int kCross = 4;
   int pad = 1;                          // units of an item are counted up to a multiple of this
   auto padded = [&](int units) -> int { return pad == 1 ? units : (units + pad - 1) / pad * pad; };

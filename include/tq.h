@@ -408,8 +408,9 @@ int tq_entropy_unpack(const tq_plan* plan, const uint8_t* lengths, int64_t n, co
 
 /* ---------------------------------------------------------------------------------------------
  * Paged 8-bit KV cache: layers that 2 to 4 bits are too coarse for, prompts, drafted tokens, for many sequences at once.  A layer's
- * tokens of a sequence are all in such a cache or all in the compressed one above: no call joins attention over both.  A cache is a pool of pages of page_tokens tokens each, all KV heads in a page; a sequence owns the pages that its row
- * of a page table names.  A block is one page of one head: its keys have one scale, its values another.
+ * tokens of a sequence are all in such a cache or all in the compressed one above: no call joins attention over both.
+ * A cache is a pool of pages of page_tokens tokens each, all KV heads in a page; a sequence owns the pages that its row of a page table
+ * names.  A block is one page of one head: its keys have one scale, its values another.
  *
  *   scale   s = 2^e with the least e >= -126 that holds the block's largest magnitude: max |x| <= M 2^e, M = 127 (TQ_I8) or 448
  *           (TQ_E4M3); 0 for a block of zeros.  Powers of two, so x / s is exact and a code is x / s rounded once, half to even:
@@ -478,8 +479,9 @@ int tq_selftest_kv8_timeout(int on);
  * the row sees fewer pages.  With qi = round(q / 2^e) in -127 .. 127 (2^e as for a block), B+ and B- the bounds in steps u s,
  *     score(page) = max over the group's heads of 2^e u s sum_c (max(qi_c, 0) B+_c + min(qi_c, 0) B-_c),
  * for scale > 0 no less than any logit of the page up to q's rounding.  Sums of integers and powers of two: scores are exact (where they
- * lie within the normal numbers of fp32), and of equal ones the lower page number is taken.  The first `first` and the last `last` pages that the row sees are always taken
- * (first + last <= k), and so, as far as k goes, is a block with scale NaN.  A query with an infinity or a NaN scores 0 everywhere.
+ * lie within the normal numbers of fp32), and of equal ones the lower page number is taken.  The first `first` and the last `last`
+ * pages that the row sees are always taken (first + last <= k), and so, as far as k goes, is a block with scale NaN.  A query with an
+ * infinity or a NaN scores 0 everywhere.
  *   lists      device out, [n, heads, k];  workspace  256-byte aligned, >= tq_kv8_select_workspace_bytes(cache, n, width)
  */
 size_t tq_kv8_select_workspace_bytes(const tq_kv8* cache, int64_t n, int width);

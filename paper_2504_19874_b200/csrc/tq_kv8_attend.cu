@@ -48,6 +48,22 @@ __device__ __forceinline__ uint32_t half2_bits(float lo, float hi) {
   const __half2 h = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&h);
 }
+// Bytes 0, 1 and bytes 2, 3 of a word of codes as pairs of fp16, exactly.  int8: the byte plus 128 is the low byte of 1024 + 128 + x.
+template <bool E4M3>
+__device__ __forceinline__ void expand(uint32_t w, uint32_t& lo, uint32_t& hi) {
+  if (E4M3) {
+    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}"
+        : "=r"(lo), "=r"(hi) : "r"(w));
+  } else {
+    w ^= 0x80808080u;
+    const uint32_t a = __byte_perm(w, 0x64646464u, 0x4140), b = __byte_perm(w, 0x64646464u, 0x4342);
+    const __half2 k = __halves2half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480));   // 1152
+    const __half2 x = __hsub2(*reinterpret_cast<const __half2*>(&a), k), y = __hsub2(*reinterpret_cast<const __half2*>(&b), k);
+    lo = *reinterpret_cast<const uint32_t*>(&x);
+    hi = *reinterpret_cast<const uint32_t*>(&y);
+  }
+}
+
 template <int W>
 __device__ __forceinline__ void load_words(const uint8_t* p, uint32_t* w) {   // W words, aligned to the largest power of two in their bytes
   if (W % 4 == 0) {

@@ -54,21 +54,6 @@ __device__ __forceinline__ float scale_log2(float s) {
   if ((u & 0x7FFFFFu) == 0u && u - 1u < 0x7F7FFFFFu) return (float)((int)(u >> 23) - 127);
   return s > 0.f ? __log2f(s) : -TQ_INF;
 }
-// Bytes 0, 1 and bytes 2, 3 of a word of codes as pairs of fp16, exactly.  int8: the byte plus 128 is the low byte of 1024 + 128 + x.
-template <bool E4M3>
-__device__ __forceinline__ void expand(uint32_t w, uint32_t& lo, uint32_t& hi) {
-  if (E4M3) {
-    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}"
-        : "=r"(lo), "=r"(hi) : "r"(w));
-  } else {
-    w ^= 0x80808080u;
-    const uint32_t a = __byte_perm(w, 0x64646464u, 0x4140), b = __byte_perm(w, 0x64646464u, 0x4342);
-    const __half2 k = __halves2half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480));   // 1152
-    const __half2 x = __hsub2(*reinterpret_cast<const __half2*>(&a), k), y = __hsub2(*reinterpret_cast<const __half2*>(&b), k);
-    lo = *reinterpret_cast<const uint32_t*>(&x);
-    hi = *reinterpret_cast<const uint32_t*>(&y);
-  }
-}
 template <typename T>
 __device__ __forceinline__ void store_out(T* p, float x);
 template <>

@@ -9,7 +9,8 @@
 // block's scale over the unit, a power of two: from 2^-15 to 1 for keys, exactly; from 2^-2 to 1 for values, as r and with it P's smallest
 // step follow the unit for rows too that do not see the block it comes from.  Blocks below that, and values of 0, are left out (masked, as keys
 // that nobody sees) and take their turn with units of their own in a second pass over the same tile: what one page holds changes nothing
-// for another.  (Pages of 16 tokens of which a third are 2^8 smaller, so that every tile takes two passes: 1,540 us for the 2,048 queries below, in place of 579.)
+// for another.  (Pages of 16 tokens of which a third are 2^8 smaller, so that every tile takes two passes: 1,540 us for the 2,048 queries
+// below, in place of 579.)
 //
 // Work.  A CTA per SM; units are (tile of 128 keys) x (block of 256 rows, fp32: 128), numbered through over blocks, heads and sequences,
 // and every CTA takes an equal run of them, so that causal triangles and ragged batches are even; runs that end inside a block leave
@@ -20,8 +21,8 @@
 //
 // Measured, one B200: 2,048 queries x 32 heads (4 per KV head, d = 128, bf16) over 16,384 tokens 581 us = 887 TFLOP/s, 0.54 of cuBLAS (595 in
 // calls made one by one); fp32 (twice the MMAs) 1,268 us; a prompt of 4,096 tokens 390 us.  A tile of 128 keys takes about 4,700 cycles,
-// its MMAs 2,060 of them and the exponentials 2,050 (both row tiles): what binds is the chain of one row tile, scores - maximum - weights - sum - next scores,
-// of which two are in flight.  Scores of 64 keys in two buffers, asked for ahead (694 us), lengthen the MMAs instead: with N = 64 they
+// its MMAs 2,060 of them and the exponentials 2,050 (both row tiles): what binds is the chain of one row tile, scores - maximum - weights -
+// sum - next scores, of which two are in flight.  Scores of 64 keys in two buffers, asked for ahead (694 us), lengthen the MMAs instead: with N = 64 they
 // are bound by the reads of the queries from shared memory.  Fewer unrolled copies of the code gained 15 %: 16 warps in four roles fetch
 // instructions from one cache.  The copies of codes in registers had to go to warps of their own for keys and values (870 -> 700 us).
 #include <algorithm>
@@ -54,9 +55,8 @@ struct Shape {
 };
 
 // Weights are 2^(s - m + kLift), and m moves when a score exceeds it by more than kSlack: rescaling O costs about as much as a tile, and
-// 2^15 is the largest power of two in fp16.  With
-// r up to 2^3 above the row's largest product of weight and scale (a whole number, and the unit of values up to 2^2 larger), what lies
-// below 2^-16 (bf16) or 2^-19 (fp32) of that may lose bits, 2^-27 or 2^-30 of it each.
+// 2^15 is the largest power of two in fp16.  With r up to 2^3 above the row's largest product of weight and scale (a whole number, and the
+// unit of values up to 2^2 larger), what lies below 2^-16 (bf16) or 2^-19 (fp32) of that may lose bits, 2^-27 or 2^-30 of it each.
 template <typename T>
 struct Range {
   static constexpr float kLift = sizeof(T) == 4 ? 8.f : 5.f, kSlack = 15.f - kLift;

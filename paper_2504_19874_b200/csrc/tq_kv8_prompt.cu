@@ -379,9 +379,9 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
     }
     tc::fence_barrier_init();
   }
-  if (warp == kMmaWarp) tc::tmem_alloc(&sh.tmem, 512);
   allow_successor();
   wait_for_predecessor();
+  if (warp == kMmaWarp) tc::tmem_alloc(&sh.tmem, 512);   // (behind the wait: a kernel ahead may have yet to allocate its own)
   tc::tc_fence_before();
   __syncthreads();
   tc::tc_fence_after();

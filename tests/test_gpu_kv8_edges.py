@@ -95,3 +95,57 @@ def test_attend_with_a_largest_number_of_rows_of_none(g, x):
     bt = Batch([90, 20, 64], d=64, page=32, dtype=E4M3, seed=17).cuda()
     starts = torch.tensor([0, 33, 34, 60], dtype=torch.int32)
     check_attend(bt, bt.randn(60, 2 * g, x), 0.15, starts, max_queries=0)
+
+
+@pytest.mark.parametrize("x", [torch.bfloat16, torch.float32])
+def test_a_captured_chunk_follows_lengths_rows_and_pages(x):
+    """Append and attention of both kinds captured once; replays see the lengths, the rows of each sequence and the table of their time."""
+    bt = Batch([100, 20, 300], heads=2, d=64, page=32, seed=51, room=3).cuda()
+    n = 90
+    K, V, Q = (torch.zeros((n, h, 64), dtype=x, device=DEV) for h in (2, 2, 8))
+    out, lse = torch.zeros_like(Q), torch.zeros((n, 8), device=DEV)
+    starts, after = torch.zeros(4, dtype=torch.int32, device=DEV), torch.zeros(3, dtype=torch.int32, device=DEV)
+    ws = workspace(tq.tq_kv8_attend_workspace_bytes(bt.cache, 3, n, 4, n))
+    side = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side), torch.cuda.graph(graph, stream=side):
+        tq.tq_kv8_append(bt.cache, bt.t, bt.n, K, V, starts=starts)
+        tq.tq_kv8_attend(bt.cache, bt.t, after, Q, 0.2, out, ws, lse=lse, starts=starts, max_queries=n)
+    for rows in ([60, 1, 20], [0, 30, 1], [1, 1, 1], [0, 0, 88]):
+        total = sum(rows)
+        s = torch.tensor([0] + rows).cumsum(0).to(torch.int32)
+        k, v, q = bt.randn(n, 2, x), bt.randn(n, 2, x), bt.randn(n, 8, x)
+        before = bt.tokens.clone()
+        for dst, src in ((K, k), (V, v), (Q, q), (starts, s), (after, before + torch.tensor(rows, dtype=torch.int32)), (bt.n, before)):
+            dst.copy_(src)
+        out.fill_(7.0), lse.fill_(7.0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        ref.append(bt.pool, bt.table, before, k, v, s)
+        bt.tokens = before + torch.tensor(rows, dtype=torch.int32)
+        want, wl, t16, t32, tl = ref.attend(bt.pool, bt.table, bt.tokens, q, 0.2, s)
+        tol = t16 if x == torch.bfloat16 else t32
+        assert bool(((out.cpu().double() - want).abs() <= tol)[:total].all()) and bool(((lse.cpu().double() - wl).abs() <= tl)[:total].all())
+        assert bool((out[total:] == 7.0).all()) and bool((lse[total:] == 7.0).all())
+
+
+def test_calls_on_two_streams_at_once():
+    """Each with a workspace of its own; results are those of calls made alone."""
+    sets = []
+    for seed in range(2):
+        bt = Batch([900, 40, 333], heads=2, d=64, page=32, dtype=E4M3 if seed else I8, seed=60 + seed).cuda()
+        starts = torch.tensor([0, 300, 301, 380], dtype=torch.int32, device=DEV)
+        Q = bt.randn(380, 8, torch.bfloat16).to(DEV)
+        ws = workspace(tq.tq_kv8_attend_workspace_bytes(bt.cache, 3, 380, 4, 300))
+        want = torch.zeros_like(Q)
+        tq.tq_kv8_attend(bt.cache, bt.t, bt.n, Q, 0.2, want, ws, starts=starts, max_queries=300)
+        sets.append((bt, starts, Q, ws, want, [torch.zeros_like(Q) for _ in range(8)], torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for i in range(8):
+        for bt, starts, Q, ws, _, outs, stream in sets:
+            with torch.cuda.stream(stream):
+                tq.tq_kv8_attend(bt.cache, bt.t, bt.n, Q, 0.2, outs[i], ws, starts=starts, max_queries=300)
+    torch.cuda.synchronize()
+    for _, _, _, _, want, outs, _ in sets:
+        assert all(torch.equal(o, want) for o in outs)
